@@ -434,6 +434,107 @@ typedef struct {
 } sgs_aux_args_t;
 sgs_status_t sgs_aux_op(int n_members, const sgs_aux_desc_t *desc, const sgs_aux_args_t *args, int grouped, void *cuda_stream);
 
+/*
+ * 8-bit floating point: codes with a scale for every block of 128 along the reduction (the paper quantises to 8-bit integers,
+ * Section 5.1 footnote; here the 8 bits are a float's and the scale is the block's own, so no calibration is needed and
+ * gradients fit too).  A matrix of R rows and C columns is held as
+ *   codes  [R][ld] bytes, e4m3 or e5m2, ld a multiple of 16 for the layers that read them
+ *   scales fp32 [ceil(C / 128)][pitch]: a line for each block of 128 columns, in it a scale for every row, or for every 128 rows
+ * and stands for code * scale.  The scales are any finite numbers; sgs_quantize_f8 writes powers of two.
+ *
+ * sgs_quantize_f8 - codes and scales of a matrix x [rows][cols] (row-wise), of its transpose, or of both from one read:
+ *   d_q [rows][ldq], d_scale [ceil(cols/128)][lds]       blocks of 1 x 128 elements (block_rows 1) or 128 x 128 (block_rows 128)
+ *   d_qt [cols][ldqt], d_scale_t [ceil(rows/128)][ldst]  the same of x^T: blocks of 128 elements of a column, or 128 x 128
+ * Row-wise codes are what a layer and the gradient of its input read (sum over x's columns); transposed codes what the gradient of
+ * its weights reads (sum over x's rows), and with block_rows 128 the transposed weights for the gradient of the input.
+ *   scale = 2^max(-126, ceil(log2(amax / FMAX))), amax the block's largest finite magnitude, FMAX 448 (e4m3) or 57344 (e5m2)
+ *   code = nearest(x / scale), ties to even; NaN and infinities become NaN
+ * d_q and d_scale, or d_qt and d_scale_t, may be NULL together.  Bytes of a row beyond its codes and scales beyond a line's are
+ * left as they were.
+ */
+typedef enum { SGS_E4M3 = 0, SGS_E5M2 = 1 } sgs_f8_format_t;
+typedef struct {
+    int rows, cols;   /* of x */
+    int dtype;        /* sgs_dtype_t of x */
+    int format;       /* sgs_f8_format_t of the codes */
+    int block_rows;   /* 1 or 128 */
+    int ldx;          /* elements from row to row of x; 0 = cols */
+    int ldq, ldqt;    /* bytes from row to row of the codes; 0 = cols resp. rows, rounded up to a multiple of 16 */
+    int lds, ldst;    /* floats from line to line of the scales; 0 = rows resp. cols, or with block_rows 128 a 128th, rounded up */
+} sgs_quantize_f8_desc_t;
+sgs_status_t sgs_quantize_f8(const sgs_quantize_f8_desc_t *desc, const void *d_x, void *d_q, float *d_scale, void *d_qt, float *d_scale_t,
+                             void *cuda_stream);
+
+/*
+ * sgs_linear_f8 - one sliced linear layer (or pointwise convolution: its pixels are the rows) on such matrices, on the 8-bit tensor
+ * cores.  Section 2.1: the layer uses the first K rows and the first C columns of the stored weights.
+ *   y[m][k] = act( sum_b sx[b][m] * sw[b][k / w_block_rows] * ( sum_{c in block b, c < C} x[m][c] * w[k][c] ) + bias[k] )
+ * Sums are fp32: the products of a block in the tensor core, the blocks in registers, in the order of c within groups that the size
+ * of the call alone decides.  y is rounded once.
+ *   d_x [M][ldx], d_sx [ceil(C/128)][ldsx] a scale per row     d_w [Kmax][ldw], d_sw [ceil(C/128)][ldsw]     d_bias [>= K] fp32 or NULL
+ *   d_y [M][ldy] fp32 or bf16
+ * The gradients of such a layer are layers of the same kind: with g the gradient of its sums, dx = g w takes g row-wise and w
+ * transposed; dw = g^T x takes both transposed, x's with a scale per row (w_block_rows 1), and an fp32 y.
+ * x and w 16-byte aligned with pitches in multiples of 16, else SGS_EUNSUPPORTED (likewise more than 2^31 - 1 tiles).
+ */
+typedef struct {
+    int M, K, C;              /* rows of x; rows (filters) and columns (channels) of w in use */
+    int Kmax, Cmax;           /* stored weights */
+    int x_format, w_format;   /* sgs_f8_format_t */
+    int w_block_rows;         /* rows of w that share a scale: 1 or 128 */
+    int y_dtype;              /* sgs_dtype_t */
+    int act;                  /* 0 none / 1 ReLU / 2 h-swish */
+    int ldx, ldw, ldy;        /* bytes, bytes, elements from row to row; 0 = C and Cmax rounded up to a multiple of 16, and K */
+    int ldsx, ldsw;           /* floats from line to line of the scales; 0 = M, and Kmax or a 128th of it, rounded up */
+} sgs_linear_f8_desc_t;
+sgs_status_t sgs_linear_f8(const sgs_linear_f8_desc_t *desc, const void *d_x, const float *d_sx, const void *d_w, const float *d_sw,
+                           const float *d_bias, void *d_y, void *cuda_stream);
+
+/*
+ * sgs_top_logits - the `top` largest of every row of logits and their classes, largest first; of equal values (-0 and 0 are equal)
+ * the lower class comes first, NaN counts as the largest.  d_z [rows][ldz], d_values fp32 and d_index int32 [rows][ldt].
+ * 1 <= top <= min(classes, SGS_TOP_LOGITS_MAX).  (What a teacher hands to sgs_distill: SubNets learn from the largest SubNet's logits.)
+ */
+#define SGS_TOP_LOGITS_MAX 256
+typedef struct {
+    int rows, classes, top;
+    int dtype;      /* sgs_dtype_t of the logits */
+    int ldz, ldt;   /* elements from row to row of z; of values and index.  0 = classes, and top */
+} sgs_top_logits_desc_t;
+sgs_status_t sgs_top_logits(const sgs_top_logits_desc_t *desc, const void *d_z, float *d_values, int *d_index, void *cuda_stream);
+
+/*
+ * sgs_distill - the distillation loss of every row of a student's logits z against a teacher's top logits, with temperature T:
+ *   p = softmax over the row's slots j of teacher[j] / T,   q = softmax over all classes of z / T
+ *   loss = T^2 * sum_j p_j * (log p_j - log q[index_j])
+ *   dz[v] = g * T * (q[v] - sum of the p_j with index_j = v),   g = grad_scale * row_scale[row]
+ * A slot whose index is outside 0 .. classes - 1, or whose teacher logit is minus infinity, is not used: lists may be of unequal length
+ * (end them with -1), and a row without any has loss 0 and gradient 0 whatever its logits.  A class named twice receives both
+ * probabilities.  Logits of minus infinity have q = 0 (a row of nothing else: q = 0 everywhere); with g = 0 a row's gradient is 0.
+ * NaN goes through.  All sums are fp32, in an order that depends on sizes, types, pitches and alignment alone; dz is rounded once.
+ *   d_z [rows][ldz] and d_dz [rows][lddz] of dtype     d_teacher fp32, d_index int32 [rows][ldt]     d_row_scale fp32 [rows] or NULL (1)
+ *   d_loss fp32 [rows]     d_stat fp32 [rows][2] or NULL: the row's largest logit and log sum exp((z - largest) / T)
+ *   d_dz NULL: the loss alone.  d_dz may be d_z with the same pitch (the gradient replaces the logits).
+ * sgs_distill_backward - dz alone, from the statistics that sgs_distill left; T, lists and logits as then.
+ * 1 <= top <= SGS_DISTILL_TOP_MAX, 0 < T < infinity, grad_scale finite.
+ */
+#define SGS_DISTILL_TOP_MAX 1024
+typedef struct {
+    int rows, classes, top;
+    int dtype;              /* sgs_dtype_t of z and dz */
+    int ldz, lddz, ldt;     /* elements from row to row; 0 = classes, classes, top */
+    float temperature;
+    float grad_scale;
+} sgs_distill_desc_t;
+sgs_status_t sgs_distill(const sgs_distill_desc_t *desc, const void *d_z, const float *d_teacher, const int *d_index, const float *d_row_scale,
+                         float *d_loss, float *d_stat, void *d_dz, void *cuda_stream);
+sgs_status_t sgs_distill_backward(const sgs_distill_desc_t *desc, const void *d_z, const float *d_teacher, const int *d_index,
+                                  const float *d_stat, const float *d_row_scale, void *d_dz, void *cuda_stream);
+/* The five calls above are asynchronous on `cuda_stream`, allocate nothing, keep nothing between calls and can be captured after a
+ * first call outside the capture (sgs_linear_f8; the others at once).  Everything passed in may be what earlier work on the stream
+ * writes; outputs must not overlap inputs (but for dz = z).  Pointers are of the current device (SGS_EINVAL for another device's
+ * and for host memory that the device cannot read). */
+
 /* Nonzero once a kernel of this process has reported that one of its bounded waits ran out (the paper has no
  * counterpart: every device-side wait of the kernels carries a time limit, after which the kernel records the fact
  * in a status word of its device, lets its copies land, frees its tensor memory and returns; calls that follow

@@ -28,6 +28,7 @@ EXPORTS = [
     "sgs_profile_read", "sgs_conv2d_sliced_static", "sgs_cache_set_candidates", "sgs_cache_set_policy",
     "sgs_sched_create", "sgs_sched_free", "sgs_sched_dims", "sgs_sched_set_table", "sgs_sched_get_table", "sgs_sched_measure",
     "sgs_sched_step", "sgs_sched_subnet", "sgs_profile_trace", "sgs_layer_name", "sgs_aux_op", "sgs_device_status_clear", "sgs_debug_expire_wait", "sgs_debug_expire_team_wait", "sgs_debug_pointwise_tiles", "sgs_debug_layer_map", "sgs_measure_fma_peak", "sgs_conv2d_sliced_i8",
+    "sgs_quantize_f8", "sgs_linear_f8", "sgs_top_logits", "sgs_distill", "sgs_distill_backward",
 ]
 
 
@@ -50,6 +51,28 @@ class AuxDesc(ctypes.Structure):
 
 class AuxArgs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("x", "y", "w", "bias", "w2", "bias2")]
+
+
+SGS_E4M3, SGS_E5M2 = 0, 1
+SGS_TOP_LOGITS_MAX, SGS_DISTILL_TOP_MAX = 256, 1024
+
+
+class QuantizeF8Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "cols", "dtype", "format", "block_rows", "ldx", "ldq", "ldqt", "lds", "ldst")]
+
+
+class LinearF8Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("M", "K", "C", "Kmax", "Cmax", "x_format", "w_format", "w_block_rows", "y_dtype", "act",
+                                             "ldx", "ldw", "ldy", "ldsx", "ldsw")]
+
+
+class TopLogitsDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "classes", "top", "dtype", "ldz", "ldt")]
+
+
+class DistillDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "classes", "top", "dtype", "ldz", "lddz", "ldt")] + [("temperature", ctypes.c_float),
+                                                                                                          ("grad_scale", ctypes.c_float)]
 
 
 class StreamOpts(ctypes.Structure):
@@ -208,6 +231,11 @@ def lib():
         L.sgs_measure_fma_peak.argtypes = [vp, vp]
         L.sgs_conv2d_sliced_i8.argtypes = [vp] * 9
         L.sgs_profile_read.argtypes = [vp, ci, vp, vp, vp, vp]
+        L.sgs_quantize_f8.argtypes = [vp] * 7
+        L.sgs_linear_f8.argtypes = [vp] * 8
+        L.sgs_top_logits.argtypes = [vp] * 5
+        L.sgs_distill.argtypes = [vp] * 9
+        L.sgs_distill_backward.argtypes = [vp] * 8
         _lib = L
     return _lib
 
@@ -241,6 +269,41 @@ def conv2d_sliced_i8(desc: ConvI8Desc, d_x: int, d_w: int, d_mult: int, d_shift:
     st = lib().sgs_conv2d_sliced_i8(ctypes.byref(desc), d_x, d_w, d_mult, d_shift, d_bias, d_res or None, d_y, stream)
     if st != SGS_OK:
         raise SgsError(st, "sgs_conv2d_sliced_i8")
+
+
+def quantize_f8(desc: QuantizeF8Desc, d_x: int, d_q: int, d_scale: int, d_qt: int = 0, d_scale_t: int = 0, stream: int = 0):
+    """sgs_quantize_f8: codes and scales of a matrix (d_q, d_scale), of its transpose (d_qt, d_scale_t), or of both."""
+    st = lib().sgs_quantize_f8(ctypes.byref(desc), d_x, d_q or None, d_scale or None, d_qt or None, d_scale_t or None, stream)
+    if st != SGS_OK:
+        raise SgsError(st, "sgs_quantize_f8")
+
+
+def linear_f8(desc: LinearF8Desc, d_x: int, d_sx: int, d_w: int, d_sw: int, d_bias: int, d_y: int, stream: int = 0):
+    """sgs_linear_f8: a sliced linear layer on 8-bit floating point operands with a scale per block of 128."""
+    st = lib().sgs_linear_f8(ctypes.byref(desc), d_x, d_sx, d_w, d_sw, d_bias or None, d_y, stream)
+    if st != SGS_OK:
+        raise SgsError(st, "sgs_linear_f8")
+
+
+def top_logits(desc: TopLogitsDesc, d_z: int, d_values: int, d_index: int, stream: int = 0):
+    """sgs_top_logits: the largest logits of every row and their classes."""
+    st = lib().sgs_top_logits(ctypes.byref(desc), d_z, d_values, d_index, stream)
+    if st != SGS_OK:
+        raise SgsError(st, "sgs_top_logits")
+
+
+def distill(desc: DistillDesc, d_z: int, d_teacher: int, d_index: int, d_row_scale: int, d_loss: int, d_stat: int = 0, d_dz: int = 0, stream: int = 0):
+    """sgs_distill: the distillation loss of every row against a teacher's top logits, with its gradient where d_dz is given."""
+    st = lib().sgs_distill(ctypes.byref(desc), d_z, d_teacher, d_index, d_row_scale or None, d_loss, d_stat or None, d_dz or None, stream)
+    if st != SGS_OK:
+        raise SgsError(st, "sgs_distill")
+
+
+def distill_backward(desc: DistillDesc, d_z: int, d_teacher: int, d_index: int, d_stat: int, d_row_scale: int, d_dz: int, stream: int = 0):
+    """sgs_distill_backward: the gradient alone, from the statistics that sgs_distill left."""
+    st = lib().sgs_distill_backward(ctypes.byref(desc), d_z, d_teacher, d_index, d_stat, d_row_scale or None, d_dz, stream)
+    if st != SGS_OK:
+        raise SgsError(st, "sgs_distill_backward")
 
 
 def device_status_clear():

@@ -2925,3 +2925,135 @@ sgs_status_t sgs_debug_pointwise_tiles(int pixels, int filters, int team, int he
 }
 
 }  // extern "C"
+
+// ---- 8-bit floating point layers and operators on logits (see sgs.h) ------------------------------------------------------
+namespace {
+
+// Whether every address (NULL: not given) is memory that kernels of the current device can use: an address of another device, or
+// of plain host memory, would fault there.
+typedef CUresult (*PointerAttributeFn)(void *, CUpointer_attribute, CUdeviceptr);
+bool on_current_device(std::initializer_list<const void *> addresses) {
+    static PointerAttributeFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        return cudaGetDriverEntryPoint("cuPointerGetAttribute", &p, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<PointerAttributeFn>(p) : nullptr;
+    }();
+    int dev = 0;
+    if (!fn || cudaGetDevice(&dev) != cudaSuccess) return false;
+    for (const void *a : addresses) {
+        int owner = -1;
+        if (a && (fn(&owner, CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL, reinterpret_cast<CUdeviceptr>(a)) != CUDA_SUCCESS || owner != dev)) return false;
+    }
+    return true;
+}
+bool is_dtype(int d) { return d == SGS_F32 || d == SGS_BF16; }
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+long long round16(long long n) { return (n + 15) / 16 * 16; }
+long long blocks128(long long n) { return (n + 127) / 128; }
+// A pitch as the descriptors give it: 0 = `dense`; false where it is less than `least`.
+bool pitch(int given, long long dense, long long least, long long *out) {
+    *out = given ? given : dense;
+    return *out >= least;
+}
+sgs_status_t launched(cudaError_t e) {
+    if (e == cudaSuccess) return SGS_OK;
+    cudaGetLastError();  // (a refused launch; later calls are not to meet it)
+    return SGS_ECUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+sgs_status_t sgs_quantize_f8(const sgs_quantize_f8_desc_t *d, const void *d_x, void *d_q, float *d_scale, void *d_qt, float *d_scale_t,
+                             void *cuda_stream) try {
+    if (!d || !d_x || !d_q != !d_scale || !d_qt != !d_scale_t || (!d_q && !d_qt)) return SGS_EINVAL;
+    if (d->rows <= 0 || d->cols <= 0 || !is_dtype(d->dtype) || (d->format != SGS_E4M3 && d->format != SGS_E5M2) || (d->block_rows != 1 && d->block_rows != 128))
+        return SGS_EINVAL;
+    QuantF8Args a;
+    a.square = d->block_rows == 128;
+    const long long lines = a.square ? blocks128(d->rows) : d->rows, lines_t = a.square ? blocks128(d->cols) : d->cols;
+    if (!pitch(d->ldx, d->cols, d->cols, &a.ldx) || !pitch(d->ldq, round16(d->cols), d->cols, &a.ldq) || !pitch(d->ldqt, round16(d->rows), d->rows, &a.ldqt) ||
+        !pitch(d->lds, lines, lines, &a.lds) || !pitch(d->ldst, lines_t, lines_t, &a.ldst))
+        return SGS_EINVAL;
+    if (!aligned(d_x, d->dtype == SGS_BF16 ? 2 : 4) || !aligned(d_scale, 4) || !aligned(d_scale_t, 4)) return SGS_EINVAL;
+    if (blocks128(d->rows) * blocks128(d->cols) > 2147483647ll) return SGS_EUNSUPPORTED;
+    if (!on_current_device({d_x, d_q, d_scale, d_qt, d_scale_t})) return SGS_EINVAL;
+    a.x = d_x; a.q = d_q; a.qt = d_qt; a.scale = d_scale; a.scale_t = d_scale_t;
+    a.rows = d->rows; a.cols = d->cols; a.bf16 = d->dtype == SGS_BF16; a.e5m2 = d->format == SGS_E5M2;
+    return launched(launch_quantize_f8(a, (cudaStream_t)cuda_stream));
+} SGS_NO_THROW
+
+sgs_status_t sgs_linear_f8(const sgs_linear_f8_desc_t *d, const void *d_x, const float *d_sx, const void *d_w, const float *d_sw,
+                           const float *d_bias, void *d_y, void *cuda_stream) try {
+    if (!d || !d_x || !d_sx || !d_w || !d_sw || !d_y) return SGS_EINVAL;
+    if (d->M <= 0 || d->K <= 0 || d->C <= 0 || d->K > d->Kmax || d->C > d->Cmax || d->x_format < SGS_E4M3 || d->x_format > SGS_E5M2 ||
+        d->w_format < SGS_E4M3 || d->w_format > SGS_E5M2 || (d->w_block_rows != 1 && d->w_block_rows != 128) || !is_dtype(d->y_dtype) || d->act < 0 || d->act > 2)
+        return SGS_EINVAL;
+    LinearF8Args a;
+    a.w_rows = d->w_block_rows == 1;
+    const long long lines = a.w_rows ? d->K : blocks128(d->K), stored = a.w_rows ? d->Kmax : blocks128(d->Kmax);
+    if (!pitch(d->ldx, round16(d->C), d->C, &a.ldx) || !pitch(d->ldw, round16(d->Cmax), d->C, &a.ldw) || !pitch(d->ldy, d->K, d->K, &a.ldy) ||
+        !pitch(d->ldsx, d->M, d->M, &a.ldsx) || !pitch(d->ldsw, stored, lines, &a.ldsw))
+        return SGS_EINVAL;
+    if (!aligned(d_sx, 4) || !aligned(d_sw, 4) || !aligned(d_bias, 4) || !aligned(d_y, d->y_dtype == SGS_BF16 ? 2 : 4)) return SGS_EINVAL;
+    if (a.ldx % 16 || a.ldw % 16 || !aligned(d_x, 16) || !aligned(d_w, 16) || blocks128(d->M) * blocks128(d->K) > 2147483647ll ||
+        d->M > 2147483647 - 512 || d->K > 2147483647 - 512 || d->C > 2147483647 - 512)
+        return SGS_EUNSUPPORTED;
+    if (!on_current_device({d_x, d_sx, d_w, d_sw, d_bias, d_y})) return SGS_EINVAL;
+    int dev = 0;
+    if (!tc_available()) return SGS_EUNSUPPORTED;
+    if (cudaGetDevice(&dev) != cudaSuccess || tc_conv_init(dev) != cudaSuccess) return SGS_ECUDA;
+    a.x = d_x; a.w = d_w; a.sx = d_sx; a.sw = d_sw; a.bias = d_bias; a.y = d_y;
+    a.M = d->M; a.K = d->K; a.C = d->C; a.x_e5m2 = d->x_format == SGS_E5M2; a.w_e5m2 = d->w_format == SGS_E5M2;
+    a.y_bf16 = d->y_dtype == SGS_BF16; a.act = d->act;
+    return launched(launch_linear_f8(a, dev, (cudaStream_t)cuda_stream));
+} SGS_NO_THROW
+
+sgs_status_t sgs_top_logits(const sgs_top_logits_desc_t *d, const void *d_z, float *d_values, int *d_index, void *cuda_stream) try {
+    static_assert(TOP_LOGITS_MAX == SGS_TOP_LOGITS_MAX && DISTILL_TOP_MAX == SGS_DISTILL_TOP_MAX, "limits of sgs.h");
+    if (!d || !d_z || !d_values || !d_index) return SGS_EINVAL;
+    if (d->rows <= 0 || d->classes <= 0 || d->top <= 0 || d->top > d->classes || d->top > TOP_LOGITS_MAX || !is_dtype(d->dtype)) return SGS_EINVAL;
+    TopArgs a;
+    if (!pitch(d->ldz, d->classes, d->classes, &a.ldz) || !pitch(d->ldt, d->top, d->top, &a.ldt)) return SGS_EINVAL;
+    if (!aligned(d_z, d->dtype == SGS_BF16 ? 2 : 4) || !aligned(d_values, 4) || !aligned(d_index, 4)) return SGS_EINVAL;
+    if (d->classes > 2147483647 - (1 << 20)) return SGS_EUNSUPPORTED;
+    if (!on_current_device({d_z, d_values, d_index})) return SGS_EINVAL;
+    a.z = d_z; a.values = d_values; a.index = d_index; a.rows = d->rows; a.classes = d->classes; a.top = d->top; a.bf16 = d->dtype == SGS_BF16;
+    return launched(launch_top_logits(a, (cudaStream_t)cuda_stream));
+} SGS_NO_THROW
+
+static sgs_status_t distill(const sgs_distill_desc_t *d, const void *d_z, const float *d_teacher, const int *d_index, const float *d_row_scale,
+                            float *d_loss, float *d_stat, void *d_dz, int backward, void *cuda_stream) {
+    if (!d || !d_z || !d_teacher || !d_index) return SGS_EINVAL;
+    if (d->rows <= 0 || d->classes <= 0 || d->top <= 0 || d->top > DISTILL_TOP_MAX || !is_dtype(d->dtype) || !(d->temperature > 0.f) ||
+        !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature) || !std::isfinite(d->grad_scale))
+        return SGS_EINVAL;
+    DistillArgs a;
+    if (!pitch(d->ldz, d->classes, d->classes, &a.ldz) || !pitch(d->lddz, d->classes, d->classes, &a.lddz) || !pitch(d->ldt, d->top, d->top, &a.ldt)) return SGS_EINVAL;
+    const size_t eb = d->dtype == SGS_BF16 ? 2 : 4;
+    if (!aligned(d_z, eb) || !aligned(d_dz, eb) || !aligned(d_teacher, 4) || !aligned(d_index, 4) || !aligned(d_row_scale, 4) || !aligned(d_loss, 4) || !aligned(d_stat, 4))
+        return SGS_EINVAL;
+    if (d_dz == d_z && a.lddz != a.ldz) return SGS_EINVAL;
+    if (d->classes > 2147483647 - (1 << 20)) return SGS_EUNSUPPORTED;
+    if (!on_current_device({d_z, d_teacher, d_index, d_row_scale, d_loss, d_stat, d_dz})) return SGS_EINVAL;
+    a.z = d_z; a.teacher = d_teacher; a.index = d_index; a.row_scale = d_row_scale; a.loss = d_loss; a.stat = d_stat; a.dz = d_dz;
+    a.rows = d->rows; a.classes = d->classes; a.top = d->top; a.bf16 = d->dtype == SGS_BF16; a.backward = backward;
+    a.temperature = d->temperature; a.grad_scale = d->grad_scale;
+    return launched(launch_distill(a, (cudaStream_t)cuda_stream));
+}
+
+sgs_status_t sgs_distill(const sgs_distill_desc_t *desc, const void *d_z, const float *d_teacher, const int *d_index, const float *d_row_scale,
+                         float *d_loss, float *d_stat, void *d_dz, void *cuda_stream) try {
+    if (!d_loss) return SGS_EINVAL;
+    return distill(desc, d_z, d_teacher, d_index, d_row_scale, d_loss, d_stat, d_dz, 0, cuda_stream);
+} SGS_NO_THROW
+
+sgs_status_t sgs_distill_backward(const sgs_distill_desc_t *desc, const void *d_z, const float *d_teacher, const int *d_index,
+                                  const float *d_stat, const float *d_row_scale, void *d_dz, void *cuda_stream) try {
+    if (!d_stat || !d_dz) return SGS_EINVAL;
+    return distill(desc, d_z, d_teacher, d_index, d_row_scale, nullptr, const_cast<float *>(d_stat), d_dz, 1, cuda_stream);
+} SGS_NO_THROW
+
+}  // extern "C"

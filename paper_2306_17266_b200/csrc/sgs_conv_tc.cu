@@ -524,6 +524,14 @@ constexpr int tc_stage_bytes(int bn) { return A_STAGE_BYTES + bn * CHUNK_C * 2; 
 
 bool tc_available() { return encode_fn() != nullptr; }
 
+bool tc_encode_bytes(CUtensorMap *m, const void *base, uint64_t cols, uint64_t rows, uint64_t pitch, uint32_t box_rows) {
+    if (!encode_fn()) return false;
+    const cuuint64_t gd[2] = {cols, rows}, gs[1] = {pitch};
+    const cuuint32_t bx[2] = {128, box_rows}, es[2] = {1, 1};
+    return encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int *tc_status_word(int device) {
     if (device < 0 || device >= 64) return nullptr;
     std::lock_guard<std::mutex> lk(g_mu);

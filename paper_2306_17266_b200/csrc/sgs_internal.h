@@ -316,4 +316,47 @@ size_t subnet_kernel_held_max();  // largest weight buffer a block can keep
 cudaError_t subnet_team_expire(int team, int block, int thread, unsigned limit_us, int *left, int *status, cudaStream_t st);  // test of the time-out path
 constexpr int SUBNET_THREADS = 512;  // of a block
 
+// ---- 8-bit floating point layers (sgs_quantize_f8.cu, sgs_linear_f8.cu) ------------------------
+struct QuantF8Args {
+    const void *x = nullptr;
+    void *q = nullptr, *qt = nullptr;
+    float *scale = nullptr, *scale_t = nullptr;
+    long long ldx = 0, ldq = 0, ldqt = 0, lds = 0, ldst = 0;
+    int rows = 0, cols = 0, bf16 = 0, e5m2 = 0, square = 0;
+};
+cudaError_t launch_quantize_f8(const QuantF8Args &a, cudaStream_t st);
+struct LinearF8Args {
+    const void *x = nullptr, *w = nullptr;
+    const float *sx = nullptr, *sw = nullptr, *bias = nullptr;
+    void *y = nullptr;
+    int M = 0, K = 0, C = 0;
+    long long ldx = 0, ldw = 0, ldy = 0, ldsx = 0, ldsw = 0;
+    int x_e5m2 = 0, w_e5m2 = 0, w_rows = 0, y_bf16 = 0, act = 0;  // w_rows: a scale for each row of w (else for 128 rows)
+};
+cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st);
+// Tensor map of a matrix of bytes: boxes of box_rows x 128 bytes, 128-byte swizzle, zeros outside.
+bool tc_encode_bytes(CUtensorMap *m, const void *base, uint64_t cols, uint64_t rows, uint64_t pitch, uint32_t box_rows);
+
+// ---- operators on logits (sgs_logits.cu) -------------------------------------------------------
+struct TopArgs {
+    const void *z = nullptr;
+    float *values = nullptr;
+    int *index = nullptr;
+    int rows = 0, classes = 0, top = 0, bf16 = 0;
+    long long ldz = 0, ldt = 0;
+};
+cudaError_t launch_top_logits(const TopArgs &a, cudaStream_t st);
+constexpr int TOP_LOGITS_MAX = 256, DISTILL_TOP_MAX = 1024;
+struct DistillArgs {
+    const void *z = nullptr;
+    const float *teacher = nullptr, *row_scale = nullptr;
+    const int *index = nullptr;
+    float *loss = nullptr, *stat = nullptr;  // stat: written by the loss, read by the backward pass
+    void *dz = nullptr;
+    int rows = 0, classes = 0, top = 0, bf16 = 0, backward = 0;
+    long long ldz = 0, lddz = 0, ldt = 0;
+    float temperature = 1.f, grad_scale = 1.f;
+};
+cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st);
+
 }  // namespace sgs

@@ -1,0 +1,221 @@
+// Block quantisation to 8-bit floating point: the codes of a matrix and of its transpose, from one read of it.
+//
+//   scale(B) = 2^e,  e = max(-126, ceil(log2(amax(B) / FMAX)))      amax: the largest finite magnitude of block B
+//   code(x)  = nearest(x / scale(B)), ties to even;  NaN and infinities become NaN
+//
+// B is 128 elements along the reduction (a row's, or in the transposed output a column's), or a square of 128 x 128.  FMAX is
+// 448 = 1.75 * 2^8 (e4m3) or 57344 = 1.75 * 2^15 (e5m2), so e follows from the exponent and mantissa bits of amax alone, without
+// a logarithm or a division, and x / scale is exact: a code is rounded once, from x itself.
+//
+// What bounds it: bytes.  A block of 256 threads takes a tile of 128 x 128: a thread holds 8 columns of 8 neighbouring rows, 16
+// threads a row, so the largest of a row is a shuffle among 16 lanes, and the 8 codes of a column and thread are one 8-byte word
+// of the transposed tile, which goes through shared memory (16 KB, units of 8 bytes swizzled by the column group: neither the
+// writes nor the 16-byte reads meet in a bank) so that the transposed codes leave in rows of 128 bytes too.
+#include "sgs_internal.h"
+#include "sgs_pdl.cuh"
+
+#include <cuda_fp8.h>
+
+namespace sgs {
+namespace {
+
+constexpr uint32_t INF_BITS = 0x7f800000u;
+
+// Power-of-two scale of a block whose largest finite magnitude has the bits `amax`: exponent field of the scale.
+__device__ __forceinline__ int scale_field(uint32_t amax, int top) {
+    const int e = (int)(amax >> 23) - 127 - top + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return max(e, -126) + 127;
+}
+__device__ __forceinline__ float scale_of(int field) { return __uint_as_float((uint32_t)field << 23); }
+__device__ __forceinline__ float inverse_of(int field) { return __uint_as_float((uint32_t)(254 - field) << 23); }
+
+template <bool E5M2> __device__ __forceinline__ uint32_t codes2(float lo, float hi) {
+    uint16_t r;
+    if (E5M2) asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <bool E5M2> __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) { return codes2<E5M2>(a, b) | codes2<E5M2>(c, d) << 16; }
+
+// 8 consecutive elements of a row as fp32, zeros from `n` on.
+__device__ __forceinline__ void load8(const float *p, int n, bool vec, float *v) {
+    if (vec && n >= 8) {
+        const float4 a = ld_act(reinterpret_cast<const float4 *>(p)), b = ld_act(reinterpret_cast<const float4 *>(p + 4));
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = j < n ? ld_act(p + j) : 0.f;
+    }
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, int n, bool vec, float *v) {
+    if (vec && n >= 8) {
+        const uint4 q = ld_act(reinterpret_cast<const uint4 *>(p));
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; j++) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = j < n ? __bfloat162float(ld_act(p + j)) : 0.f;
+    }
+}
+// `n` of the bytes of one or two words.
+__device__ __forceinline__ void store_bytes(uint8_t *p, uint32_t lo, uint32_t hi, int n) {
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+        if (j < n) p[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+}
+
+struct QuantParams {
+    const void *x;
+    uint8_t *q, *qt;
+    float *scale, *scale_t;
+    long long ldx, ldq, ldqt, lds, ldst;
+    int rows, cols, col_tiles;
+    int vec_x, vec_q, vec_qt;  // 16-byte (q: 8-byte) accesses allowed
+};
+
+template <typename T, bool E5M2, bool SQUARE, bool ROWS, bool TRANSPOSED>
+__global__ void __launch_bounds__(256) quantize_f8_kernel(const QuantParams p) {
+    __shared__ __align__(16) uint8_t tile[TRANSPOSED ? 128 * 128 : 16];
+    __shared__ uint32_t col_max[TRANSPOSED && !SQUARE ? 16 : 1][128];
+    __shared__ uint32_t warp_max[8];
+    constexpr int TOP = E5M2 ? 15 : 8;
+    const int t = threadIdx.x, l = t & 15, g = t >> 4;  // columns 8 l .., rows 8 g ..
+    const int ct = (int)(blockIdx.x % (unsigned)p.col_tiles), rt = (int)(blockIdx.x / (unsigned)p.col_tiles);
+    const int r0 = rt * 128 + 8 * g, c0 = ct * 128 + 8 * l;
+    const int n = min(8, p.cols - c0);  // (may be negative)
+    pdl_launch_dependents();
+    pdl_wait();
+    float v[8][8];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const bool in = r0 + i < p.rows && n > 0;
+        load8(static_cast<const T *>(p.x) + (in ? (long long)(r0 + i) * p.ldx + c0 : 0), in ? n : 0, p.vec_x, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) most = max(most, __float_as_uint(v[i][j]) & 0x7fffffffu);
+    // A tile with a NaN or an infinity (rare): they become NaN, and the scales are those of the other elements.
+    const bool odd = __syncthreads_or(most >= INF_BITS);
+    auto size = [&](float f) -> uint32_t {
+        const uint32_t a = __float_as_uint(f) & 0x7fffffffu;
+        return odd && a >= INF_BITS ? 0u : a;
+    };
+    if (odd) {
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                if ((__float_as_uint(v[i][j]) & 0x7fffffffu) >= INF_BITS) v[i][j] = __uint_as_float(0x7fc00000u);
+                most = max(most, size(v[i][j]));
+            }
+    }
+    int square = 0;
+    if (SQUARE) {
+        most = __reduce_max_sync(0xffffffffu, most);
+        if ((t & 31) == 0) warp_max[t >> 5] = most;
+        __syncthreads();
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) most = max(most, warp_max[i]);
+        square = scale_field(most, TOP);
+        if (t == 0) {
+            if (ROWS) p.scale[(long long)ct * p.lds + rt] = scale_of(square);
+            if (TRANSPOSED) p.scale_t[(long long)rt * p.ldst + ct] = scale_of(square);
+        }
+    }
+    if (ROWS) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            int field = square;
+            if (!SQUARE) {
+                uint32_t a = 0;
+#pragma unroll
+                for (int j = 0; j < 8; j++) a = max(a, size(v[i][j]));
+#pragma unroll
+                for (int o = 8; o; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+                field = scale_field(a, TOP);
+                if (l == 0 && r0 + i < p.rows) p.scale[(long long)ct * p.lds + r0 + i] = scale_of(field);
+            }
+            const float inv = inverse_of(field);
+            const uint32_t lo = codes4<E5M2>(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
+            const uint32_t hi = codes4<E5M2>(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+            if (r0 + i < p.rows && n > 0) {
+                uint8_t *dst = p.q + (long long)(r0 + i) * p.ldq + c0;
+                if (p.vec_q && n == 8) *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+                else store_bytes(dst, lo, hi, n);
+            }
+        }
+    }
+    if (TRANSPOSED) {
+        if (!SQUARE) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                uint32_t a = 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++) a = max(a, size(v[i][j]));
+                col_max[g][8 * l + j] = a;
+            }
+            __syncthreads();
+            if (t < 128) {
+                uint32_t a = 0;
+#pragma unroll
+                for (int i = 0; i < 16; i++) a = max(a, col_max[i][t]);
+                const int field = scale_field(a, TOP);
+                if (ct * 128 + t < p.cols) p.scale_t[(long long)rt * p.ldst + ct * 128 + t] = scale_of(field);
+                col_max[0][t] = (uint32_t)(254 - field) << 23;
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const float inv = SQUARE ? inverse_of(square) : __uint_as_float(col_max[0][8 * l + j]);
+            const uint32_t lo = codes4<E5M2>(v[0][j] * inv, v[1][j] * inv, v[2][j] * inv, v[3][j] * inv);
+            const uint32_t hi = codes4<E5M2>(v[4][j] * inv, v[5][j] * inv, v[6][j] * inv, v[7][j] * inv);
+            *reinterpret_cast<uint2 *>(tile + (8 * l + j) * 128 + ((g ^ l) * 8)) = make_uint2(lo, hi);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int c = (t >> 3) + 32 * i, k = t & 7, s = c >> 3;  // column, 16-byte piece, its swizzle
+            const uint4 w = *reinterpret_cast<const uint4 *>(tile + c * 128 + (((2 * k) ^ s) & ~1) * 8);
+            const uint4 u = s & 1 ? make_uint4(w.z, w.w, w.x, w.y) : w;
+            const int row = rt * 128 + 16 * k, m = min(16, p.rows - row);
+            if (ct * 128 + c < p.cols && m > 0) {
+                uint8_t *dst = p.qt + (long long)(ct * 128 + c) * p.ldqt + row;
+                if (p.vec_qt && m == 16) *reinterpret_cast<uint4 *>(dst) = u;
+                else { store_bytes(dst, u.x, u.y, m); store_bytes(dst + 8, u.z, u.w, m - 8); }
+            }
+        }
+    }
+}
+
+template <typename T, bool E5M2, bool SQUARE> cudaError_t launch_sides(const QuantParams &p, unsigned blocks, cudaStream_t st) {
+    if (p.q && p.qt) return launch_pdl(quantize_f8_kernel<T, E5M2, SQUARE, true, true>, dim3(blocks), dim3(256), 0, st, 1, p);
+    if (p.q) return launch_pdl(quantize_f8_kernel<T, E5M2, SQUARE, true, false>, dim3(blocks), dim3(256), 0, st, 1, p);
+    return launch_pdl(quantize_f8_kernel<T, E5M2, SQUARE, false, true>, dim3(blocks), dim3(256), 0, st, 1, p);
+}
+template <typename T> cudaError_t launch_type(const QuantParams &p, int e5m2, int square, unsigned blocks, cudaStream_t st) {
+    if (e5m2) return square ? launch_sides<T, true, true>(p, blocks, st) : launch_sides<T, true, false>(p, blocks, st);
+    return square ? launch_sides<T, false, true>(p, blocks, st) : launch_sides<T, false, false>(p, blocks, st);
+}
+
+}  // namespace
+
+cudaError_t launch_quantize_f8(const QuantF8Args &a, cudaStream_t st) {
+    QuantParams p;
+    p.x = a.x; p.q = static_cast<uint8_t *>(a.q); p.qt = static_cast<uint8_t *>(a.qt); p.scale = a.scale; p.scale_t = a.scale_t;
+    p.ldx = a.ldx; p.ldq = a.ldq; p.ldqt = a.ldqt; p.lds = a.lds; p.ldst = a.ldst;
+    p.rows = a.rows; p.cols = a.cols; p.col_tiles = (a.cols + 127) / 128;
+    const size_t eb = a.bf16 ? 2 : 4;
+    p.vec_x = ((reinterpret_cast<uintptr_t>(a.x) | (size_t)a.ldx * eb) & 15) == 0;
+    p.vec_q = ((reinterpret_cast<uintptr_t>(a.q) | (size_t)a.ldq) & 7) == 0;
+    p.vec_qt = ((reinterpret_cast<uintptr_t>(a.qt) | (size_t)a.ldqt) & 15) == 0;
+    const unsigned blocks = (unsigned)((long long)p.col_tiles * ((a.rows + 127) / 128));
+    return a.bf16 ? launch_type<__nv_bfloat16>(p, a.e5m2, a.square, blocks, st) : launch_type<float>(p, a.e5m2, a.square, blocks, st);
+}
+
+}  // namespace sgs
