@@ -1,4 +1,11 @@
 // Operators on logits: the k largest of every row, and the distillation loss against a teacher's top logits with its gradient.
+//
+// Both read rows of some thousand to some hundred thousand logits and are bound by bytes where there are many rows and by a chain of
+// latencies where there are few.  Hence for both: a row is one block's, or the blocks of a cluster take contiguous parts of it and meet
+// through distributed shared memory where the rows alone do not fill the GPU; 16-byte loads, four in flight a thread, from the first
+// aligned element of a row on (rows of an odd pitch start anywhere); a second pass over the same row instead of keeping it (three
+// blocks of an SM hold about 1 MB of rows at a time between the two passes on all SMs together, which stays in the 126 MB L2: HBM
+// sees one read).
 #include "sgs_internal.h"
 #include "sgs_pdl.cuh"
 
@@ -15,65 +22,209 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162f
 __device__ __forceinline__ void from_float(float *p, float v) { *p = v; }
 __device__ __forceinline__ void from_float(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
+// 16 bytes of a row.
+template <typename T> struct Vec { static constexpr int N = 16 / (int)sizeof(T); };
+__device__ __forceinline__ void unpack(const uint4 &q, float (&v)[4]) {
+    v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+}
+__device__ __forceinline__ void unpack(const uint4 &q, float (&v)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int j = 0; j < 4; j++) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+}
+__device__ __forceinline__ uint4 pack(const float (&v)[4]) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&v)[8]) {
+    uint4 q;
+    __nv_bfloat162 *b = reinterpret_cast<__nv_bfloat162 *>(&q);
+#pragma unroll
+    for (int j = 0; j < 4; j++) b[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+    return q;
+}
+
+// How a row of V elements splits: `head` elements up to the first 16-byte boundary, vectors, the rest; the vectors are divided among
+// the blocks of the cluster, the head and the rest (fewer than two vectors together) belong to block 0.
+struct Split {
+    int head, first, last, edges;  // vectors first .. last - 1 are this block's
+    long long tail;                // first element behind the vectors
+    __device__ long long edge(int e) const { return e < head ? e : tail + (e - head); }
+};
+template <typename T> __device__ __forceinline__ Split split_row(const T *row, int V, int part, int parts) {
+    constexpr int N = Vec<T>::N;
+    Split s;
+    s.head = min(V, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(T));
+    const int n = (V - s.head) / N;
+    s.first = (int)((long long)n * part / parts);
+    s.last = (int)((long long)n * (part + 1) / parts);
+    s.tail = s.head + (long long)n * N;
+    s.edges = part == 0 ? s.head + (int)(V - s.tail) : 0;
+    return s;
+}
+
+// ---- clusters along z ------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t peer_addr(const void *p, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float2 peer_ld2(uint32_t a) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void peer_st64(uint32_t a, uint64_t v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory"); }
+
+// Blocks a row: as many as give every SM two blocks, but none less than `least` bytes.
+int parts_for(long long rows, double row_bytes, double least) {
+    int parts = 1;
+    while (parts < 8 && rows * parts < 2ll * sm_count() && row_bytes / (2 * parts) >= least) parts *= 2;
+    return parts;
+}
+
 // ---------------------------------------------------------------------------------------------
 // Top logits.  A logit's rank is that of its 64-bit word: an order-preserving key of the value above the complement of its index, so
 // that no two words are equal, larger values come first and of equal values (-0 and 0 are) the lower index.  NaN is the largest.
+//
+// A row (or part) in two passes: the k-th largest of the threads' own maxima bounds the k-th largest logit from below, and few more
+// than k logits reach it; these are collected and ranked by counting.  Rows where too many reach it (many equal values) find the
+// k-th largest word eight bits at a time.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);  // (-0 becomes 0)
     if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }  // (NaN: 0x7fffffff)
+__device__ __forceinline__ uint64_t word_of(float v, uint32_t i) { return (uint64_t)key_of(v) << 32 | (uint32_t)~i; }
+// Maximum that is NaN if one operand is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float vec_max(const uint4 &q, const float *) {
+    return max_nan(max_nan(__uint_as_float(q.x), __uint_as_float(q.y)), max_nan(__uint_as_float(q.z), __uint_as_float(q.w)));
+}
+__device__ __forceinline__ float vec_max(const uint4 &q, const __nv_bfloat16 *) {
+    const uint32_t m = max_nan2(max_nan2(q.x, q.y), max_nan2(q.z, q.w));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+}
 
-constexpr int TOP_THREADS = 1024, TOP_CAP = 1024;
+constexpr int TOP_CAP = 1024;
+struct TopParams {
+    const void *z;
+    float *values;
+    int *index;
+    int V, k, parts;
+    long long ldz, ldt;
+};
 
-template <typename T> __global__ void __launch_bounds__(TOP_THREADS) top_logits_kernel(const T *z, float *values, int *index, int V, int k, long long ldz, long long ldt) {
+template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(const TopParams p) {
+    constexpr int N = Vec<T>::N, U = 4;
     __shared__ uint64_t cand[TOP_CAP];
-    __shared__ int n_cand;
-    __shared__ int hist[256];
+    __shared__ uint64_t joined[8 * TOP_LOGITS_MAX];  // block 0: the parts' words
+    __shared__ int n_cand, want_s;
     __shared__ uint64_t prefix_s;
-    __shared__ int want_s;
+    __shared__ int hist[256];
+    const int t = threadIdx.x, part = (int)blockIdx.z, k = p.k;
     pdl_launch_dependents();
     pdl_wait();
-    const T *row = z + (long long)blockIdx.x * ldz;
-    const int t = threadIdx.x;
-    // The k-th largest of the threads' own maxima is a lower bound of the k-th largest logit.
-    uint32_t most = 0;
-    for (int i = t; i < V; i += TOP_THREADS) most = max(most, key_of(to_float(ld_act(row + i))));
-    uint32_t least = 0;
-    if (V > TOP_CAP)
-        for (int b = 31; b >= 0; b--) {
-            const uint32_t trial = least | (1u << b);
-            if (__syncthreads_count(most >= trial) >= k) least = trial;
+    const T *row = static_cast<const T *>(p.z) + (long long)blockIdx.x * p.ldz;
+    const Split s = split_row(row, p.V, part, p.parts);
+    const uint4 *vec = reinterpret_cast<const uint4 *>(row + s.head);
+    // Calls f(vector, its first element) for this thread's vectors, f1(value, element) for its share of the edges.
+    auto walk = [&](auto f, auto f1) {
+        for (int i = s.first + t; i < s.last; i += U * THREADS) {
+            uint4 q[U];
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (i + u * THREADS < s.last) q[u] = ld_act(vec + i + u * THREADS);
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (i + u * THREADS < s.last) f(q[u], (uint32_t)(s.head + (i + u * THREADS) * N));
         }
+        if (t < s.edges) { const long long e = s.edge(t); f1(to_float(ld_act(row + e)), (uint32_t)e); }
+    };
+    // Short parts, where vectors would leave threads without any logit: element by element.
+    const long long e0 = part == 0 ? 0 : s.head + (long long)s.first * N, e1 = part == p.parts - 1 ? p.V : s.head + (long long)s.last * N;
+    const bool brief = e1 - e0 <= 2 * N * THREADS;
+    const bool edges_apart = p.parts > 1;  // (then the edges are block 0's: the ranges above leave the tail to it)
+    auto each = [&](auto f1) {
+        const long long last = edges_apart ? s.head + (long long)s.last * N : p.V;
+        for (long long i = (edges_apart ? s.head + (long long)s.first * N : 0) + t; i < last; i += THREADS) f1(to_float(ld_act(row + i)), (uint32_t)i);
+        if (edges_apart && t < s.edges) { const long long e = s.edge(t); f1(to_float(ld_act(row + e)), (uint32_t)e); }
+    };
+    uint32_t most = 0;  // (below every key)
+    if (brief) each([&](float v, uint32_t) { most = max(most, key_of(v)); });
+    else {
+        float m = NEG_INF;
+        walk([&](const uint4 &q, uint32_t) { m = max_nan(m, vec_max(q, (const T *)nullptr)); }, [&](float v, uint32_t) { m = max_nan(m, v); });
+        most = key_of(m);
+    }
+    uint32_t least = 0;
+    for (int b = 31; b >= (sizeof(T) == 2 ? 16 : 0); b--) {  // (the lower half of a bf16's key tells nothing: zeros, or ones below zero)
+        const uint32_t trial = least | (1u << b);
+        const int count = __syncthreads_count(most >= trial);
+        if (count >= k) least = trial;
+        if (count == k) break;
+    }
     if (t == 0) n_cand = 0;
     __syncthreads();
-    for (int i = t; i < V; i += TOP_THREADS) {
-        const uint32_t key = key_of(to_float(ld_act(row + i)));
+    auto take = [&](float v, uint32_t i) {
+        const uint32_t key = key_of(v);
         if (key >= least) {
             const int at = atomicAdd(&n_cand, 1);  // (any order: the ranks below do not depend on it)
             if (at < TOP_CAP) cand[at] = (uint64_t)key << 32 | (uint32_t)~i;
         }
-    }
+    };
+    if (brief) each(take);
+    else
+        walk([&](const uint4 &q, uint32_t i) {
+            if (key_of(vec_max(q, (const T *)nullptr)) < least) return;
+            float v[N];
+            unpack(q, v);
+#pragma unroll
+            for (int j = 0; j < N; j++) take(v[j], i + j);
+        }, take);
     __syncthreads();
     int n = n_cand;
     if (n > TOP_CAP) {
-        // Too many candidates (many equal values): the k-th largest word itself, eight bits at a time.
+        // The k-th largest word itself.
         uint64_t prefix = 0;
         int want = k;
         for (int shift = 56; shift >= 0; shift -= 8) {
             if (t < 256) hist[t] = 0;
             __syncthreads();
-            for (int i0 = 0; i0 < V; i0 += TOP_THREADS) {
-                const int i = i0 + t;
-                int digit = -1;
-                if (i < V) {
-                    const uint64_t w = (uint64_t)key_of(to_float(ld_act(row + i))) << 32 | (uint32_t)~i;
-                    if (shift == 56 || (w >> (shift + 8)) == (prefix >> (shift + 8))) digit = (int)(w >> shift) & 255;
+            // (runs of one digit, which is what brings rows here, are added up by the thread that meets them)
+            int held = -1, count = 0;
+            auto tally = [&](float v, uint32_t i) {
+                const uint64_t w = word_of(v, i);
+                if (shift < 56 && (w >> (shift + 8)) != (prefix >> (shift + 8))) return;
+                const int d = (int)(w >> shift) & 255;
+                if (d != held) {
+                    if (count) atomicAdd(&hist[held], count);
+                    held = d;
+                    count = 0;
                 }
-                const unsigned same = __match_any_sync(0xffffffffu, digit);
-                if (digit >= 0 && (int)(__ffs(same) - 1) == (t & 31)) atomicAdd(&hist[digit], __popc(same));
-            }
+                count++;
+            };
+            if (brief) each(tally);
+            else
+                walk([&](const uint4 &q, uint32_t i) {
+                    float v[N];
+                    unpack(q, v);
+#pragma unroll
+                    for (int j = 0; j < N; j++) tally(v[j], i + j);
+                }, tally);
+            if (count) atomicAdd(&hist[held], count);
             __syncthreads();
             if (t == 0) {
                 int d = 255, left = want;
@@ -87,157 +238,288 @@ template <typename T> __global__ void __launch_bounds__(TOP_THREADS) top_logits_
         }
         if (t == 0) n_cand = 0;
         __syncthreads();
-        for (int i = t; i < V; i += TOP_THREADS) {
-            const uint64_t w = (uint64_t)key_of(to_float(ld_act(row + i))) << 32 | (uint32_t)~i;
+        auto keep = [&](float v, uint32_t i) {
+            const uint64_t w = word_of(v, i);
             if (w >= prefix) cand[atomicAdd(&n_cand, 1)] = w;  // (exactly k of them)
-        }
+        };
+        if (brief) each(keep);
+        else
+            walk([&](const uint4 &q, uint32_t i) {
+                if (key_of(vec_max(q, (const T *)nullptr)) < (uint32_t)(prefix >> 32)) return;
+                float v[N];
+                unpack(q, v);
+#pragma unroll
+                for (int j = 0; j < N; j++) keep(v[j], i + j);
+            }, keep);
         __syncthreads();
         n = n_cand;
     }
-    if (t < n) {
-        const uint64_t w = cand[t];
+    float *values = p.values + (long long)blockIdx.x * p.ldt;
+    int *index = p.index + (long long)blockIdx.x * p.ldt;
+    auto write = [&](int rank, uint64_t w) {
+        values[rank] = value_of((uint32_t)(w >> 32));
+        index[rank] = (int)~(uint32_t)w;
+    };
+    if (p.parts == 1) {
+        for (int c = t; c < n; c += THREADS) {
+            const uint64_t w = cand[c];
+            int rank = 0;
+            for (int i = 0; i < n; i++) rank += cand[i] > w;
+            if (rank < k) write(rank, w);
+        }
+        return;
+    }
+    if (part == 0)
+        for (int c = t; c < p.parts * k; c += THREADS) joined[c] = 0;  // (no logit's word)
+    cluster_arrive();
+    cluster_wait();
+    for (int c = t; c < n; c += THREADS) {
+        const uint64_t w = cand[c];
         int rank = 0;
         for (int i = 0; i < n; i++) rank += cand[i] > w;
-        if (rank < k) {
-            const int i = (int)~(uint32_t)w;
-            values[(long long)blockIdx.x * ldt + rank] = to_float(ld_act(row + i));
-            index[(long long)blockIdx.x * ldt + rank] = i;
+        if (rank < k) peer_st64(peer_addr(&joined[part * k + rank], 0), w);
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (part) return;
+    for (int c = t; c < p.parts * k; c += THREADS) {
+        const uint64_t w = joined[c];
+        // own part's words are sorted: the rank there is known, of another part's it is the number of larger ones
+        int rank = c % k;
+        if (!w) continue;
+        for (int q = 0; q < p.parts; q++) {
+            if (q == c / k) continue;
+            int lo = 0, hi = k;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (joined[q * k + mid] > w) lo = mid + 1;
+                else hi = mid;
+            }
+            rank += lo;
         }
+        if (rank < k) write(rank, w);
     }
 }
 
 // ---------------------------------------------------------------------------------------------
-// Distillation
+// Distillation.  One pass keeps a running maximum and a sum of exponentials relative to it, a second writes the gradient.
 // ---------------------------------------------------------------------------------------------
-constexpr int DIS_THREADS = 512;
-
-template <typename Op> __device__ __forceinline__ float block_reduce(float v, float *buf, Op op) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = buf[0];
-    for (int i = 1; i < (int)(blockDim.x >> 5); i++) v = op(v, buf[i]);
-    return v;
+// 2^x; results below the normal range are 0.
+__device__ __forceinline__ float pow2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
-__device__ __forceinline__ float fmax_op(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float add_op(float a, float b) { return a + b; }
+// (largest, sum of 2^(a (v - largest))) of two sets; of an empty set or one of -infinities: (-infinity, 0).
+__device__ __forceinline__ float2 join(float2 p, float2 q, float a) {
+    const float m = fmaxf(p.x, q.x), b = m == NEG_INF ? 0.f : m;
+    return make_float2(m, p.y * pow2((p.x - b) * a) + q.y * pow2((q.x - b) * a));
+}
+template <int THREADS> __device__ __forceinline__ void block_join(float2 &u, float2 &v, float a, float4 *buf) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        u = join(u, make_float2(__shfl_xor_sync(0xffffffffu, u.x, o), __shfl_xor_sync(0xffffffffu, u.y, o)), a);
+        v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)), a);
+    }
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = make_float4(u.x, u.y, v.x, v.y);
+    __syncthreads();
+    u = v = make_float2(NEG_INF, 0.f);
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; i++) {
+        u = join(u, make_float2(buf[i].x, buf[i].y), a);
+        v = join(v, make_float2(buf[i].z, buf[i].w), a);
+    }
+}
 
-template <typename T> struct DisParams {
-    const T *z;
-    T *dz;
+struct DisParams {
+    const void *z;
+    void *dz;
     const float *teacher, *row_scale;
     const int *index;
     float *loss, *stat;
-    int V, k, backward;
+    int V, k, backward, parts;
     long long ldz, lddz, ldt;
     float inv_t, temperature, grad_scale;
 };
 
-template <typename T> __global__ void __launch_bounds__(DIS_THREADS) distill_kernel(const DisParams<T> p) {
-    __shared__ float buf[32];
+template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const DisParams p) {
+    constexpr int N = Vec<T>::N, U = 4;
+    __shared__ float4 buf[THREADS / 32];
+    __shared__ float sums[THREADS / 32];
+    __shared__ __align__(8) float2 mine;
     __shared__ int at[DISTILL_TOP_MAX];
     __shared__ float prob[DISTILL_TOP_MAX], zl[DISTILL_TOP_MAX];
+    const int t = threadIdx.x, V = p.V, k = p.k, part = (int)blockIdx.z;
+    const long long r = blockIdx.x;
     pdl_launch_dependents();
     pdl_wait();
-    const int t = threadIdx.x, V = p.V, k = p.k;
-    const long long r = blockIdx.x;
-    const T *row = p.z + r * p.ldz;
+    const T *row = static_cast<const T *>(p.z) + r * p.ldz;
     const float a = p.inv_t * LOG2E;
-    // the teacher's distribution over the slots in use
-    float tmax = NEG_INF;
-    bool used_any = false, nan_any = false;
-    for (int j = t; j < k; j += DIS_THREADS) {
+    const Split s = split_row(row, V, part, p.parts);
+    const uint4 *vec = reinterpret_cast<const uint4 *>(row + s.head);
+
+    // the teacher's list (every block of the row reads it): slots not in use have at = -1
+    float2 teach = make_float2(NEG_INF, 0.f), stud = make_float2(NEG_INF, 0.f);
+    for (int j = t; j < k; j += THREADS) {
         int i = ld_act(p.index + r * p.ldt + j);
         const float v = ld_act(p.teacher + r * p.ldt + j);
         if (i < 0 || i >= V || v == NEG_INF) i = -1;
         at[j] = i;
         prob[j] = v;
-        if (i >= 0) { tmax = fmaxf(tmax, v); used_any = true; nan_any |= v != v; }
+        zl[j] = i >= 0 ? to_float(ld_act(row + i)) : 0.f;
+        if (i >= 0) teach = join(teach, make_float2(v == v ? v : NEG_INF, v == v ? 1.f : v), a);
     }
-    const bool used = __syncthreads_or(used_any);
-    (void)nan_any;
-    tmax = block_reduce(tmax, buf, fmax_op);
-    if (tmax == NEG_INF) tmax = 0.f;  // (all NaN)
-    float tsum = 0.f;
-    for (int j = t; j < k; j += DIS_THREADS) {
-        const float e = at[j] >= 0 ? exp2f((prob[j] - tmax) * a) : 0.f;
-        zl[j] = at[j] >= 0 ? to_float(ld_act(row + at[j])) : 0.f;
-        tsum += e;
+    if (!p.backward) {
+        float m = NEG_INF, sum = 0.f;
+        auto add = [&](auto &v) {
+            float most = v[0];
+#pragma unroll
+            for (int j = 1; j < (int)(sizeof(v) / sizeof(float)); j++) most = fmaxf(most, v[j]);
+            if (most > m) {
+                sum *= pow2((m - most) * a);
+                m = most;
+            }
+            const float b = m == NEG_INF ? 0.f : m;
+#pragma unroll
+            for (int j = 0; j < (int)(sizeof(v) / sizeof(float)); j++) sum += pow2((v[j] - b) * a);
+        };
+        for (int i = s.first + t; i < s.last; i += U * THREADS) {
+            uint4 q[U];
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (i + u * THREADS < s.last) q[u] = ld_act(vec + i + u * THREADS);
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (i + u * THREADS < s.last) {
+                    float v[N];
+                    unpack(q[u], v);
+                    add(v);
+                }
+        }
+        if (t < s.edges) {
+            float v[1] = {to_float(ld_act(row + s.edge(t)))};
+            add(v);
+        }
+        stud = make_float2(m, sum);
     }
-    tsum = block_reduce(tsum, buf, add_op);
-    // the student's statistics
-    float zmax = NEG_INF, logsum;
+    block_join<THREADS>(stud, teach, a, buf);
+    const bool used = !(teach.x == NEG_INF && teach.y == 0.f);  // (a sum of NaN is one: slots are in use)
+    if (p.parts > 1 && !p.backward) {
+        if (t == 0) mine = stud;
+        cluster_arrive();
+        cluster_wait();
+        stud = make_float2(NEG_INF, 0.f);
+        for (int q = 0; q < p.parts; q++) stud = join(stud, peer_ld2(peer_addr(&mine, q)), a);
+        cluster_arrive();  // (nobody leaves before all have read: the wait is at the end)
+    }
+    float zmax = stud.x, logsum = logf(stud.y);
     if (p.backward) {
         zmax = ld_act(p.stat + 2 * r);
         logsum = ld_act(p.stat + 2 * r + 1);
-    } else {
-        for (int i = t; i < V; i += DIS_THREADS) zmax = fmaxf(zmax, to_float(ld_act(row + i)));
-        zmax = block_reduce(zmax, buf, fmax_op);
-        const float base = zmax == NEG_INF ? 0.f : zmax;
-        float s = 0.f;
-        for (int i = t; i < V; i += DIS_THREADS) s += exp2f((to_float(ld_act(row + i)) - base) * a);
-        logsum = logf(block_reduce(s, buf, add_op));
     }
     const float base = zmax == NEG_INF ? 0.f : zmax, off = zmax == NEG_INF ? 0.f : logsum;
-    const float log_tsum = logf(tsum);
-    if (!p.backward) {
+    const float tmax = teach.x == NEG_INF ? 0.f : teach.x, tsum = teach.y;
+    if (!p.backward && part == 0) {
+        const float log_tsum = logf(tsum);
         float loss = 0.f;
-        for (int j = t; j < k; j += DIS_THREADS)
-            if (at[j] >= 0) {
+        for (int j = t; j < k; j += THREADS)
+            if (at[j] >= 0) {  // (the thread's own slots: no barrier needed)
                 // T (log p - log q), with differences of logits as they are: masks of the type's lowest value do not overflow
                 const float term = (prob[j] - tmax) - (zl[j] - base) + p.temperature * (off - log_tsum);
-                const float pj = exp2f((prob[j] - tmax) * a) / tsum;
+                const float pj = pow2((prob[j] - tmax) * a) / tsum;
                 if (!(pj <= 0.f)) loss += pj * term;
             }
-        loss = block_reduce(loss, buf, add_op);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+        if ((t & 31) == 0) sums[t >> 5] = loss;
+        __syncthreads();
         if (t == 0) {
+            loss = 0.f;
+#pragma unroll
+            for (int i = 0; i < THREADS / 32; i++) loss += sums[i];
             p.loss[r] = used ? loss * p.temperature : 0.f;
             if (p.stat) { p.stat[2 * r] = zmax; p.stat[2 * r + 1] = logsum; }
         }
     }
-    if (!p.dz) return;
-    __syncthreads();
-    for (int j = t; j < k; j += DIS_THREADS) prob[j] = at[j] >= 0 ? exp2f((prob[j] - tmax) * a) / tsum : 0.f;
-    T *out = p.dz + r * p.lddz;
-    const float c = used ? p.grad_scale * p.temperature * (p.row_scale ? ld_act(p.row_scale + r) : 1.f) : 0.f;
-    const float off2 = off * LOG2E;
-    if (c == 0.f) {
-        for (int i = t; i < V; i += DIS_THREADS) from_float(out + i, 0.f);
-        return;
+    if (p.dz) {
+        T *out = static_cast<T *>(p.dz) + r * p.lddz;
+        const float c = used ? p.grad_scale * p.temperature * (p.row_scale ? ld_act(p.row_scale + r) : 1.f) : 0.f;
+        const float off2 = off * LOG2E;
+        const bool same = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+        auto grad = [&](float v) { return c * pow2((v - base) * a - off2); };
+        for (int j = t; j < k; j += THREADS) prob[j] = at[j] >= 0 ? pow2((prob[j] - tmax) * a) / tsum : 0.f;
+        for (int i = s.first + t; i < s.last; i += U * THREADS) {
+            uint4 q[U];
+            if (c != 0.f) {
+#pragma unroll
+                for (int u = 0; u < U; u++)
+                    if (i + u * THREADS < s.last) q[u] = ld_act(vec + i + u * THREADS);
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (i + u * THREADS < s.last) {
+                    float v[N];
+                    if (c != 0.f) {
+                        unpack(q[u], v);
+#pragma unroll
+                        for (int j = 0; j < N; j++) v[j] = grad(v[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < N; j++) v[j] = 0.f;
+                    }
+                    T *dst = out + s.head + (long long)(i + u * THREADS) * N;
+                    if (same) *reinterpret_cast<uint4 *>(dst) = pack(v);
+                    else {
+#pragma unroll
+                        for (int j = 0; j < N; j++) from_float(dst + j, v[j]);
+                    }
+                }
+        }
+        if (t < s.edges) {
+            const long long e = s.edge(t);
+            from_float(out + e, c != 0.f ? grad(to_float(ld_act(row + e))) : 0.f);
+        }
+        __syncthreads();
+        // the named classes of this part, a warp a slot: q less the probability of all slots with that class, rounded once
+        const long long e0 = s.head + (long long)s.first * N, e1 = s.head + (long long)s.last * N;
+        for (int j = t >> 5; j < k; j += THREADS / 32) {
+            const int i = at[j];
+            if (i < 0 || c == 0.f || !((i >= e0 && i < e1) || (part == 0 && (i < s.head || i >= s.tail)))) continue;
+            float sum = 0.f;
+            for (int l = t & 31; l < k; l += 32) sum += at[l] == i ? prob[l] : 0.f;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if ((t & 31) == 0) from_float(out + i, c * (pow2((zl[j] - base) * a - off2) - sum));
+        }
     }
-    for (int i = t; i < V; i += DIS_THREADS) from_float(out + i, c * exp2f((to_float(ld_act(row + i)) - base) * a - off2));
-    __syncthreads();
-    for (int j = t; j < k; j += DIS_THREADS) {
-        if (at[j] < 0) continue;
-        float sum = 0.f;
-        for (int i = 0; i < k; i++) sum += at[i] == at[j] ? prob[i] : 0.f;
-        from_float(out + at[j], c * (exp2f((zl[j] - base) * a - off2) - sum));
-    }
+    if (p.parts > 1 && !p.backward) cluster_wait();
 }
 
-template <typename T> cudaError_t launch_distill_type(const DistillArgs &a, cudaStream_t st) {
-    DisParams<T> p;
-    p.z = static_cast<const T *>(a.z); p.dz = static_cast<T *>(a.dz);
-    p.teacher = a.teacher; p.row_scale = a.row_scale; p.index = a.index; p.loss = a.loss; p.stat = a.stat;
-    p.V = a.classes; p.k = a.top; p.backward = a.backward; p.ldz = a.ldz; p.lddz = a.lddz; p.ldt = a.ldt;
-    p.inv_t = 1.f / a.temperature; p.temperature = a.temperature; p.grad_scale = a.grad_scale;
-    return launch_pdl(distill_kernel<T>, dim3((unsigned)a.rows), dim3(DIS_THREADS), 0, st, 1, p);
+template <typename T, int THREADS> cudaError_t launch_distill_threads(const DisParams &p, int rows, cudaStream_t st) {
+    return launch_pdl(distill_kernel<T, THREADS>, dim3((unsigned)rows, 1, (unsigned)p.parts), dim3(THREADS), 0, st, (unsigned)p.parts, p);
 }
 
 }  // namespace
 
 cudaError_t launch_top_logits(const TopArgs &a, cudaStream_t st) {
-    if (a.bf16)
-        return launch_pdl(top_logits_kernel<__nv_bfloat16>, dim3((unsigned)a.rows), dim3(TOP_THREADS), 0, st, 1, static_cast<const __nv_bfloat16 *>(a.z), a.values,
-                          a.index, a.classes, a.top, a.ldz, a.ldt);
-    return launch_pdl(top_logits_kernel<float>, dim3((unsigned)a.rows), dim3(TOP_THREADS), 0, st, 1, static_cast<const float *>(a.z), a.values, a.index,
-                      a.classes, a.top, a.ldz, a.ldt);
+    TopParams p;
+    p.z = a.z; p.values = a.values; p.index = a.index; p.V = a.classes; p.k = a.top; p.ldz = a.ldz; p.ldt = a.ldt;
+    p.parts = parts_for(a.rows, (double)a.classes * (a.bf16 ? 2 : 4), 16384);
+    const dim3 grid((unsigned)a.rows, 1, (unsigned)p.parts);
+    if (a.bf16) return launch_pdl(top_logits_kernel<__nv_bfloat16, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p);
+    return launch_pdl(top_logits_kernel<float, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p);
 }
 
 cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
-    return a.bf16 ? launch_distill_type<__nv_bfloat16>(a, st) : launch_distill_type<float>(a, st);
+    DisParams p;
+    p.z = a.z; p.dz = a.dz; p.teacher = a.teacher; p.row_scale = a.row_scale; p.index = a.index; p.loss = a.loss; p.stat = a.stat;
+    p.V = a.classes; p.k = a.top; p.backward = a.backward; p.ldz = a.ldz; p.lddz = a.lddz; p.ldt = a.ldt;
+    p.inv_t = 1.f / a.temperature; p.temperature = a.temperature; p.grad_scale = a.grad_scale;
+    const double bytes = (double)a.classes * (a.bf16 ? 2 : 4);
+    p.parts = parts_for(a.rows, bytes, 16384);
+    if (bytes <= 16384)
+        return a.bf16 ? launch_distill_threads<__nv_bfloat16, 256>(p, a.rows, st) : launch_distill_threads<float, 256>(p, a.rows, st);
+    return a.bf16 ? launch_distill_threads<__nv_bfloat16, 512>(p, a.rows, st) : launch_distill_threads<float, 512>(p, a.rows, st);
 }
 
 }  // namespace sgs
