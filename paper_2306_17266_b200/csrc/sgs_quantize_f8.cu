@@ -37,27 +37,102 @@ template <bool E5M2> __device__ __forceinline__ uint32_t codes2(float lo, float 
 }
 template <bool E5M2> __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) { return codes2<E5M2>(a, b) | codes2<E5M2>(c, d) << 16; }
 
-// 8 consecutive elements of a row as fp32, zeros from `n` on.
-__device__ __forceinline__ void load8(const float *p, int n, bool vec, float *v) {
-    if (vec && n >= 8) {
-        const float4 a = ld_act(reinterpret_cast<const float4 *>(p)), b = ld_act(reinterpret_cast<const float4 *>(p + 4));
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
+// 8 consecutive elements of a row as they lie in memory, zeros from `n` on: the tiles stay in this form in registers (half the
+// registers for bf16), and the largest magnitude of two bf16 is one 16-bit SIMD maximum.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ float at(int j) const { return __uint_as_float(w[j]); }
+    __device__ __forceinline__ uint32_t most() const {
+        uint32_t m = 0;
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = j < n ? ld_act(p + j) : 0.f;
+        for (int j = 0; j < 8; j++) m = max(m, w[j] & 0x7fffffffu);
+        return m;
     }
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, int n, bool vec, float *v) {
-    if (vec && n >= 8) {
-        const uint4 q = ld_act(reinterpret_cast<const uint4 *>(p));
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    __device__ __forceinline__ void set_nan() {
 #pragma unroll
-        for (int j = 0; j < 4; j++) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = j < n ? __bfloat162float(ld_act(p + j)) : 0.f;
+        for (int j = 0; j < 8; j++) w[j] = (w[j] & 0x7fffffffu) >= INF_BITS ? 0x7fc00000u : w[j];
     }
-}
+    __device__ __forceinline__ uint32_t most_finite() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) m = max(m, (w[j] & 0x7fffffffu) >= INF_BITS ? 0u : w[j] & 0x7fffffffu);
+        return m;
+    }
+    __device__ __forceinline__ void load(const float *p, int n, bool vec) {
+        if (vec && n >= 8) {
+            const uint4 a = ld_act(reinterpret_cast<const uint4 *>(p)), b = ld_act(reinterpret_cast<const uint4 *>(p) + 1);
+            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++) w[j] = j < n ? __float_as_uint(ld_act(p + j)) : 0u;
+        }
+    }
+};
+template <> struct Eight<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ float at(int j) const { return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16); }
+    static __device__ __forceinline__ uint32_t wide(uint32_t m) { return max(m & 0xffff0000u, m << 16); }
+    __device__ __forceinline__ uint32_t most() const {
+        return wide(__vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu)));
+    }
+    __device__ __forceinline__ void set_nan() {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t odd = __vcmpgeu2(w[j] & 0x7fff7fffu, 0x7f807f80u);
+            w[j] = (w[j] & ~odd) | (0x7fc07fc0u & odd);
+        }
+    }
+    __device__ __forceinline__ uint32_t most_finite() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t v = w[j] & 0x7fff7fffu;
+            m = __vmaxu2(m, v & ~__vcmpgeu2(v, 0x7f807f80u));
+        }
+        return wide(m);
+    }
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, int n, bool vec) {
+        if (vec && n >= 8) {
+            const uint4 q = ld_act(reinterpret_cast<const uint4 *>(p));
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                w[j] = (2 * j < n ? (uint32_t)ld_act(reinterpret_cast<const unsigned short *>(p) + 2 * j) : 0u) |
+                       (2 * j + 1 < n ? (uint32_t)ld_act(reinterpret_cast<const unsigned short *>(p) + 2 * j + 1) << 16 : 0u);
+        }
+    }
+};
+// The largest magnitudes of each of the 8 columns of some rows.
+template <typename T> struct EightMax;
+template <> struct EightMax<float> {
+    uint32_t m[8] = {};
+    __device__ __forceinline__ void add(const Eight<float> &e) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) m[j] = max(m[j], e.w[j] & 0x7fffffffu);
+    }
+    __device__ __forceinline__ void add_finite(const Eight<float> &e) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) m[j] = max(m[j], (e.w[j] & 0x7fffffffu) >= INF_BITS ? 0u : e.w[j] & 0x7fffffffu);
+    }
+    __device__ __forceinline__ uint32_t bits(int j) const { return m[j]; }
+};
+template <> struct EightMax<__nv_bfloat16> {
+    uint32_t m[4] = {};
+    __device__ __forceinline__ void add(const Eight<__nv_bfloat16> &e) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) m[j] = __vmaxu2(m[j], e.w[j] & 0x7fff7fffu);
+    }
+    __device__ __forceinline__ void add_finite(const Eight<__nv_bfloat16> &e) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t v = e.w[j] & 0x7fff7fffu;
+            m[j] = __vmaxu2(m[j], v & ~__vcmpgeu2(v, 0x7f807f80u));
+        }
+    }
+    __device__ __forceinline__ uint32_t bits(int j) const { return j & 1 ? m[j >> 1] & 0xffff0000u : m[j >> 1] << 16; }
+};
 // `n` of the bytes of one or two words.
 __device__ __forceinline__ void store_bytes(uint8_t *p, uint32_t lo, uint32_t hi, int n) {
 #pragma unroll
@@ -74,8 +149,51 @@ struct QuantParams {
     int vec_x, vec_q, vec_qt;  // 16-byte (q: 8-byte) accesses allowed
 };
 
+template <typename T, bool E5M2> __device__ __forceinline__ uint2 codes8(const Eight<T> &e, float inv) {
+    return make_uint2(codes4<E5M2>(e.at(0) * inv, e.at(1) * inv, e.at(2) * inv, e.at(3) * inv), codes4<E5M2>(e.at(4) * inv, e.at(5) * inv, e.at(6) * inv, e.at(7) * inv));
+}
+__device__ __forceinline__ uint32_t half_warp_max(uint32_t a) {
+#pragma unroll
+    for (int o = 8; o; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+    return a;
+}
+
+// Row-wise codes alone, a scale per 128 elements: 16 threads take a block of each of four neighbouring rows; nothing is shared.
+constexpr int QROWS = 4;
+template <typename T, bool E5M2> __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantParams p) {
+    constexpr int TOP = E5M2 ? 15 : 8;
+    const int t = threadIdx.x, l = t & 15, g = t >> 4;
+    const int ct = (int)(blockIdx.x % (unsigned)p.col_tiles), rt = (int)(blockIdx.x / (unsigned)p.col_tiles);
+    const int r0 = rt * (16 * QROWS) + QROWS * g, c0 = ct * 128 + 8 * l;
+    const int n = min(8, p.cols - c0);
+    pdl_launch_dependents();
+    pdl_wait();
+    Eight<T> v[QROWS];
+#pragma unroll
+    for (int i = 0; i < QROWS; i++) {
+        const bool in = r0 + i < p.rows && n > 0;
+        v[i].load(static_cast<const T *>(p.x) + (in ? (long long)(r0 + i) * p.ldx + c0 : 0), in ? n : 0, p.vec_x);
+    }
+#pragma unroll
+    for (int i = 0; i < QROWS; i++) {
+        uint32_t a = half_warp_max(v[i].most());
+        if (__any_sync(0xffffffffu, a >= INF_BITS)) {  // (rare; for both half-warps, whose shuffles are one instruction)
+            a = half_warp_max(v[i].most_finite());
+            v[i].set_nan();
+        }
+        const int field = scale_field(a, TOP);
+        const uint2 q = codes8<T, E5M2>(v[i], inverse_of(field));
+        if (r0 + i < p.rows && n > 0) {
+            uint8_t *dst = p.q + (long long)(r0 + i) * p.ldq + c0;
+            if (p.vec_q && n == 8) *reinterpret_cast<uint2 *>(dst) = q;
+            else store_bytes(dst, q.x, q.y, n);
+            if (l == 0) p.scale[(long long)ct * p.lds + r0 + i] = scale_of(field);
+        }
+    }
+}
+
 template <typename T, bool E5M2, bool SQUARE, bool ROWS, bool TRANSPOSED>
-__global__ void __launch_bounds__(256) quantize_f8_kernel(const QuantParams p) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) quantize_f8_kernel(const QuantParams p) {
     __shared__ __align__(16) uint8_t tile[TRANSPOSED ? 128 * 128 : 16];
     __shared__ uint32_t col_max[TRANSPOSED && !SQUARE ? 16 : 1][128];
     __shared__ uint32_t warp_max[8];
@@ -86,32 +204,24 @@ __global__ void __launch_bounds__(256) quantize_f8_kernel(const QuantParams p) {
     const int n = min(8, p.cols - c0);  // (may be negative)
     pdl_launch_dependents();
     pdl_wait();
-    float v[8][8];
+    Eight<T> v[8];
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const bool in = r0 + i < p.rows && n > 0;
-        load8(static_cast<const T *>(p.x) + (in ? (long long)(r0 + i) * p.ldx + c0 : 0), in ? n : 0, p.vec_x, v[i]);
+        v[i].load(static_cast<const T *>(p.x) + (in ? (long long)(r0 + i) * p.ldx + c0 : 0), in ? n : 0, p.vec_x);
     }
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-#pragma unroll
-        for (int j = 0; j < 8; j++) most = max(most, __float_as_uint(v[i][j]) & 0x7fffffffu);
+    for (int i = 0; i < 8; i++) most = max(most, v[i].most());
     // A tile with a NaN or an infinity (rare): they become NaN, and the scales are those of the other elements.
     const bool odd = __syncthreads_or(most >= INF_BITS);
-    auto size = [&](float f) -> uint32_t {
-        const uint32_t a = __float_as_uint(f) & 0x7fffffffu;
-        return odd && a >= INF_BITS ? 0u : a;
-    };
     if (odd) {
         most = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-#pragma unroll
-            for (int j = 0; j < 8; j++) {
-                if ((__float_as_uint(v[i][j]) & 0x7fffffffu) >= INF_BITS) v[i][j] = __uint_as_float(0x7fc00000u);
-                most = max(most, size(v[i][j]));
-            }
+        for (int i = 0; i < 8; i++) {
+            most = max(most, v[i].most_finite());
+            v[i].set_nan();
+        }
     }
     int square = 0;
     if (SQUARE) {
@@ -127,54 +237,49 @@ __global__ void __launch_bounds__(256) quantize_f8_kernel(const QuantParams p) {
             if (TRANSPOSED) p.scale_t[(long long)rt * p.ldst + ct] = scale_of(square);
         }
     }
+    if (TRANSPOSED && !SQUARE) {
+        EightMax<T> cm;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (odd) cm.add_finite(v[i]);
+            else cm.add(v[i]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j += 4)
+            *reinterpret_cast<uint4 *>(&col_max[g][8 * l + j]) = make_uint4(cm.bits(j), cm.bits(j + 1), cm.bits(j + 2), cm.bits(j + 3));
+        __syncthreads();
+        if (t < 128) {
+            uint32_t a = 0;
+#pragma unroll
+            for (int i = 0; i < 16; i++) a = max(a, col_max[i][t]);
+            const int field = scale_field(a, TOP);
+            if (ct * 128 + t < p.cols) p.scale_t[(long long)rt * p.ldst + ct * 128 + t] = scale_of(field);
+            col_max[0][t] = (uint32_t)(254 - field) << 23;
+        }
+    }
     if (ROWS) {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             int field = square;
             if (!SQUARE) {
-                uint32_t a = 0;
-#pragma unroll
-                for (int j = 0; j < 8; j++) a = max(a, size(v[i][j]));
-#pragma unroll
-                for (int o = 8; o; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
-                field = scale_field(a, TOP);
+                field = scale_field(half_warp_max(odd ? v[i].most_finite() : v[i].most()), TOP);
                 if (l == 0 && r0 + i < p.rows) p.scale[(long long)ct * p.lds + r0 + i] = scale_of(field);
             }
-            const float inv = inverse_of(field);
-            const uint32_t lo = codes4<E5M2>(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-            const uint32_t hi = codes4<E5M2>(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+            const uint2 q = codes8<T, E5M2>(v[i], inverse_of(field));
             if (r0 + i < p.rows && n > 0) {
                 uint8_t *dst = p.q + (long long)(r0 + i) * p.ldq + c0;
-                if (p.vec_q && n == 8) *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
-                else store_bytes(dst, lo, hi, n);
+                if (p.vec_q && n == 8) *reinterpret_cast<uint2 *>(dst) = q;
+                else store_bytes(dst, q.x, q.y, n);
             }
         }
     }
     if (TRANSPOSED) {
-        if (!SQUARE) {
-#pragma unroll
-            for (int j = 0; j < 8; j++) {
-                uint32_t a = 0;
-#pragma unroll
-                for (int i = 0; i < 8; i++) a = max(a, size(v[i][j]));
-                col_max[g][8 * l + j] = a;
-            }
-            __syncthreads();
-            if (t < 128) {
-                uint32_t a = 0;
-#pragma unroll
-                for (int i = 0; i < 16; i++) a = max(a, col_max[i][t]);
-                const int field = scale_field(a, TOP);
-                if (ct * 128 + t < p.cols) p.scale_t[(long long)rt * p.ldst + ct * 128 + t] = scale_of(field);
-                col_max[0][t] = (uint32_t)(254 - field) << 23;
-            }
-            __syncthreads();
-        }
+        if (!SQUARE) __syncthreads();
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const float inv = SQUARE ? inverse_of(square) : __uint_as_float(col_max[0][8 * l + j]);
-            const uint32_t lo = codes4<E5M2>(v[0][j] * inv, v[1][j] * inv, v[2][j] * inv, v[3][j] * inv);
-            const uint32_t hi = codes4<E5M2>(v[4][j] * inv, v[5][j] * inv, v[6][j] * inv, v[7][j] * inv);
+            const uint32_t lo = codes4<E5M2>(v[0].at(j) * inv, v[1].at(j) * inv, v[2].at(j) * inv, v[3].at(j) * inv);
+            const uint32_t hi = codes4<E5M2>(v[4].at(j) * inv, v[5].at(j) * inv, v[6].at(j) * inv, v[7].at(j) * inv);
             *reinterpret_cast<uint2 *>(tile + (8 * l + j) * 128 + ((g ^ l) * 8)) = make_uint2(lo, hi);
         }
         __syncthreads();
@@ -195,7 +300,10 @@ __global__ void __launch_bounds__(256) quantize_f8_kernel(const QuantParams p) {
 
 template <typename T, bool E5M2, bool SQUARE> cudaError_t launch_sides(const QuantParams &p, unsigned blocks, cudaStream_t st) {
     if (p.q && p.qt) return launch_pdl(quantize_f8_kernel<T, E5M2, SQUARE, true, true>, dim3(blocks), dim3(256), 0, st, 1, p);
-    if (p.q) return launch_pdl(quantize_f8_kernel<T, E5M2, SQUARE, true, false>, dim3(blocks), dim3(256), 0, st, 1, p);
+    if (p.q) {
+        if constexpr (SQUARE) return launch_pdl(quantize_f8_kernel<T, E5M2, true, true, false>, dim3(blocks), dim3(256), 0, st, 1, p);
+        else return launch_pdl(quantize_rows_kernel<T, E5M2>, dim3((unsigned)((long long)p.col_tiles * ((p.rows + 16 * QROWS - 1) / (16 * QROWS)))), dim3(256), 0, st, 1, p);
+    }
     return launch_pdl(quantize_f8_kernel<T, E5M2, SQUARE, false, true>, dim3(blocks), dim3(256), 0, st, 1, p);
 }
 template <typename T> cudaError_t launch_type(const QuantParams &p, int e5m2, int square, unsigned blocks, cudaStream_t st) {
