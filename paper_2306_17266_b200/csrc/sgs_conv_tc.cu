@@ -524,6 +524,14 @@ constexpr int tc_stage_bytes(int bn) { return A_STAGE_BYTES + bn * CHUNK_C * 2; 
 
 bool tc_available() { return encode_fn() != nullptr; }
 
+bool tc_encode_output(CUtensorMap *m, void *base, uint64_t cols, uint64_t rows, uint64_t pitch, bool bf16, uint32_t box_cols, uint32_t box_rows) {
+    if (!encode_fn()) return false;
+    const cuuint64_t gd[2] = {cols, rows}, gs[1] = {pitch};
+    const cuuint32_t bx[2] = {box_cols, box_rows}, es[2] = {1, 1};
+    return encode_fn()(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool tc_encode_bytes(CUtensorMap *m, const void *base, uint64_t cols, uint64_t rows, uint64_t pitch, uint32_t box_rows) {
     if (!encode_fn()) return false;
     const cuuint64_t gd[2] = {cols, rows}, gs[1] = {pitch};

@@ -336,6 +336,8 @@ struct LinearF8Args {
 cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st);
 // Tensor map of a matrix of bytes: boxes of box_rows x 128 bytes, 128-byte swizzle, zeros outside.
 bool tc_encode_bytes(CUtensorMap *m, const void *base, uint64_t cols, uint64_t rows, uint64_t pitch, uint32_t box_rows);
+// Tensor map of an output matrix (bf16 or fp32), for stores of boxes of 64-byte rows with the 64-byte swizzle.
+bool tc_encode_output(CUtensorMap *m, void *base, uint64_t cols, uint64_t rows, uint64_t pitch, bool bf16, uint32_t box_cols, uint32_t box_rows);
 
 // ---- operators on logits (sgs_logits.cu) -------------------------------------------------------
 struct TopArgs {

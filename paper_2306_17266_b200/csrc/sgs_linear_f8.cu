@@ -14,216 +14,371 @@ namespace {
 
 constexpr int F8_BLOCK = 128;                       // reduction steps of a scale, of a pipeline stage and of a 128-byte swizzle row
 constexpr int F8_A_BYTES = TILE_M * F8_BLOCK;
-constexpr int F8_SUM_WARPS = 8, F8_THREADS = 64 + 32 * F8_SUM_WARPS;
+constexpr int F8_SUM_WARPS = 8, F8_THREADS = 128 + 32 * F8_SUM_WARPS;
+constexpr int F8_RING = 160 * 1024;                 // operand stages
+constexpr int F8_SCALES = 8;                        // blocks whose scales are in shared memory or on their way
+constexpr int F8_OUT = 2048;                        // an output box of a warp: 32 rows x 64 bytes
 
 struct F8Params {
-    CUtensorMap tmX, tmW;
+    CUtensorMap tmX, tmW, tmY;
     const float *sx, *sw, *bias;
     void *y;
     int *status;
     long long ldsx, ldsw, ldy;
     int M, K, C, blocks;        // blocks of the reduction
     int m_tiles, n_tiles;
-    int act, y_bf16, vec_y;     // vec_y: 16-byte stores allowed
+    int act, y_bf16;
+    int bulk_y;                 // columns of y that the copy unit may write: all where rows end on 16 bytes (it cuts boxes off there, not at the column)
     uint32_t formats;           // operand formats at their places in the instruction descriptor
 };
 
-__device__ __forceinline__ void umma_f8_if(uint32_t on, uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(on)
-        : "memory");
+template <int CTAS> __device__ __forceinline__ void umma_f8_if(uint32_t on, uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+    if (CTAS == 2)
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(on)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(on)
+            : "memory");
 }
-__device__ __forceinline__ void tma_load_2d_if(uint32_t on, uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
-    asm volatile(
-        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-        "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}"
-        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(on)
-        : "memory");
+// Commit of the MMAs issued so far; of a pair's to the barrier at this place in both blocks.
+template <int CTAS> __device__ __forceinline__ void commit_if(uint32_t on, uint32_t bar) {
+    if (CTAS == 2)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+            "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}" ::"r"(bar), "r"(on), "h"((uint16_t)3) : "memory");
+    else umma_commit_if(on, bar);
+}
+// Copy of a tile into this block's shared memory; `bar` may be the pair's first block's.
+template <int CTAS> __device__ __forceinline__ void tma_load_2d_if(uint32_t on, uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
+    if (CTAS == 2)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];\n\t}"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(on)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(on)
+            : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ uint32_t block_addr(uint32_t saddr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+    return r;
+}
+// Arrival at a barrier of either block, behind tensor-memory loads alone.  (A release at cluster scope waits for all of the thread's
+// memory operations: 1000 to 1700 clocks here, three times a block's MMAs.)
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory"); }
+__device__ __forceinline__ void pair_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+template <int CTAS> __device__ __forceinline__ void f8_tmem_alloc(uint32_t *dst, uint32_t cols) {
+    if (CTAS == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else tmem_alloc(dst, cols);
+}
+template <int CTAS> __device__ __forceinline__ void f8_tmem_dealloc(uint32_t addr, uint32_t cols) {
+    if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+    else tmem_dealloc(addr, cols);
+}
+__device__ __forceinline__ void copy_float(float *dst, const float *src, bool in) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+// Waits for this warp's tensor-memory loads; the values named are the ones that they bring.
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
+                   "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]),
+                   "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 ::"memory");
 }
 
-// One output row's `n` consecutive columns o[0..] (n at most N).
+// One output row's `n` consecutive columns o[0..] (n at most N), where the copy unit cannot write them: rows of y that do not start or, in the last columns, do not end on 16 bytes.
 template <int N> __device__ __forceinline__ void store_row(const F8Params &p, long long at, const float *o, int n) {
-    if (p.y_bf16) {
-        __nv_bfloat16 *y = static_cast<__nv_bfloat16 *>(p.y) + at;
 #pragma unroll
-        for (int j = 0; j < N; j += 8) {
-            if (p.vec_y && j + 8 <= n) {
-                uint4 v;
-                __nv_bfloat162 *b = reinterpret_cast<__nv_bfloat162 *>(&v);
-#pragma unroll
-                for (int i = 0; i < 4; i++) b[i] = __floats2bfloat162_rn(o[j + 2 * i], o[j + 2 * i + 1]);
-                *reinterpret_cast<uint4 *>(y + j) = v;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if (j + i < n) y[j + i] = __float2bfloat16_rn(o[j + i]);
-            }
+    for (int j = 0; j < N; j++)
+        if (j < n) {
+            if (p.y_bf16) static_cast<__nv_bfloat16 *>(p.y)[at + j] = __float2bfloat16_rn(o[j]);
+            else static_cast<float *>(p.y)[at + j] = o[j];
         }
-    } else {
-        float *y = static_cast<float *>(p.y) + at;
-#pragma unroll
-        for (int j = 0; j < N; j += 4) {
-            if (p.vec_y && j + 4 <= n) *reinterpret_cast<float4 *>(y + j) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-            else {
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    if (j + i < n) y[j + i] = o[j + i];
-            }
-        }
-    }
 }
 
-// A tile of 128 rows of x (lanes of the tensor memory) x BN rows of w (columns).  Warp 0 loads, warp 1 issues, eight warps add up:
-// a quadrant of the lanes and half of the columns each.  Two accumulators: the tensor core sums a block into one while the
-// warps take the other.
-template <int BN, bool W_ROWS>
-__global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_constant__ F8Params p, const int stages) {
-    constexpr int STAGE = F8_A_BYTES + BN * F8_BLOCK, COLS = BN / 2, CHUNK = 32;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full_bar[TC_MAX_STAGES], empty_bar[TC_MAX_STAGES], acc_full[2], acc_empty[2];
-    __shared__ __align__(16) float col_scale[W_ROWS ? 2 : 1][W_ROWS ? BN : 4];
-    __shared__ uint32_t tmem_base_s;
-    __shared__ int abort_s;
-    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+// A tile is 128 rows of x a block (lanes of the tensor memory) x BN rows of w (columns); CTAS = 2: the blocks of a cluster of two share
+// a tile of 256 rows, each holds its rows of x and half of the rows of w, and the first one issues the MMAs for both.
+// Warp 0 loads, warp 1 issues, warps 4..11 add up: a quadrant of the lanes and half of the columns each.  512 / BN accumulators: the
+// tensor core sums a block into one while the warps take another, and into the next tile's while they write this one's.
+template <int CTAS, int BN, bool W_ROWS>
+__global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_constant__ F8Params p) {
+    constexpr int B_ROWS = BN / CTAS, STAGE = F8_A_BYTES + B_ROWS * F8_BLOCK, STAGES = F8_RING / STAGE, NACC = 512 / BN, COLS = BN / 2;
+    struct Shared {
+        alignas(16) float row_scale[F8_SCALES][TILE_M], col_scale[F8_SCALES][W_ROWS ? BN : 4];  // (not W_ROWS: one for each half of the columns)
+        alignas(16) float bias[BN];
+        alignas(8) uint64_t full[STAGES], empty[STAGES], acc_full[NACC], acc_empty[NACC], sc_full[F8_SCALES], sc_empty[F8_SCALES];
+        uint32_t tmem_base;
+        int abort;
+    };
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Shared &sh = *reinterpret_cast<Shared *>(smem + F8_RING + F8_SUM_WARPS * 2 * F8_OUT);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    volatile int *abort_flag = &abort_s;
-    const int mt = (int)(blockIdx.x % (unsigned)p.m_tiles), nt = (int)(blockIdx.x / (unsigned)p.m_tiles);
-    const int m0 = mt * TILE_M, f0 = nt * BN;
+    const int rank = CTAS == 2 ? (int)(blockIdx.x & 1) : 0, group = (int)blockIdx.x / CTAS, groups = (int)gridDim.x / CTAS;
+    volatile int *abort_flag = &sh.abort;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < stages; s++) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int i = 0; i < 2; i++) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], F8_SUM_WARPS); }
-        abort_s = 0;
+        for (int s = 0; s < STAGES; s++) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int i = 0; i < NACC; i++) { mbar_init(&sh.acc_full[i], 1); mbar_init(&sh.acc_empty[i], F8_SUM_WARPS * CTAS); }
+        for (int i = 0; i < F8_SCALES; i++) { mbar_init(&sh.sc_full[i], 32); mbar_init(&sh.sc_empty[i], F8_SUM_WARPS); }
+        sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(&tmem_base_s, 2 * BN);
+    if (warp == 1) f8_tmem_alloc<CTAS>(&sh.tmem_base, 512);
     tc_fence_before();
     __syncthreads();
+    if (CTAS == 2) pair_sync();
     tc_fence_after();
-    const uint32_t tmem_base = tmem_base_s;
+    const uint32_t tmem_base = sh.tmem_base;
     pdl_launch_dependents();
     pdl_wait();
     const uint32_t ring = smem_u32(smem);
-    const int blocks = p.blocks;
+    const int blocks = p.blocks, tiles = p.m_tiles * p.n_tiles;
+    // Tiles go by strips of 8 along the rows: the tiles at work at a time share what they read of both operands.
+    auto place = [&](int tile, int *m0, int *f0) {
+        const int strip = 8 * p.n_tiles, g = tile / strip, rest = tile - g * strip, wide = min(8, p.m_tiles - 8 * g);
+        *m0 = ((8 * g + rest % wide) * CTAS + rank) * TILE_M;
+        *f0 = rest / wide * BN;
+    };
 
-    if (warp == 0) {
-        const uint32_t on = elect_one(), full0 = smem_u32(full_bar);
-        int s = 0;
-        uint32_t phase = 0;
-        for (int b = 0; b < blocks; b++) {
-            if (b >= stages && !__all_sync(0xffffffffu, mbar_wait(&empty_bar[s], phase ^ 1, abort_flag))) break;
-            const uint32_t sa = ring + (uint32_t)(s * STAGE), fb = full0 + (uint32_t)(s * 8);
-            mbar_expect_tx_if(on, fb, STAGE);
-            tma_load_2d_if(on, sa, &p.tmX, fb, b * F8_BLOCK, m0);
-            tma_load_2d_if(on, sa + F8_A_BYTES, &p.tmW, fb, b * F8_BLOCK, f0);
-            if (++s == stages) { s = 0; phase ^= 1; }
-        }
-    } else if (warp == 1) {
-        const uint32_t on = elect_one(), d_tmem = uniform(tmem_base), empty0 = smem_u32(empty_bar), acc0 = smem_u32(acc_full);
-        const int n_mma = min(BN, (p.K - f0 + 15) & ~15);
-        // instruction descriptor: fp32 accumulator at bit 4, operand formats at bits 7 / 10, N >> 3 at bit 17, M >> 4 at bit 24
-        const uint32_t idesc = (1u << 4) | p.formats | ((uint32_t)(n_mma >> 3) << 17) | ((uint32_t)(TILE_M >> 4) << 24);
-        int s = 0;
-        uint32_t phase = 0;
-        for (int b = 0; b < blocks; b++) {
-            const int a = b & 1;
-            if (b >= 2 && !__all_sync(0xffffffffu, mbar_wait(&acc_empty[a], (uint32_t)((b >> 1) - 1) & 1, abort_flag))) break;
-            if (!__all_sync(0xffffffffu, mbar_wait(&full_bar[s], phase, abort_flag))) break;
-            tc_fence_after();
-            const int steps = min(4, (p.C - b * F8_BLOCK + 31) / 32);
-            const uint32_t sa = ring + (uint32_t)(s * STAGE);
-            const uint64_t da = smem_desc_sw128(sa), db = smem_desc_sw128(sa + F8_A_BYTES);
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0) {
+            const uint32_t on = elect_one(), full0 = CTAS == 2 ? block_addr(smem_u32(sh.full), 0) : smem_u32(sh.full), first = rank == 0 ? on : 0;
+            int s = 0;
+            uint32_t phase = 1;  // (the first pass over the ring finds it empty)
+            bool ok = true;
+            for (int tile = group; ok && tile < tiles; tile += groups) {
+                int m0, f0;
+                place(tile, &m0, &f0);
+                for (int b = 0; b < blocks; b++) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(&sh.empty[s], phase, abort_flag))) { ok = false; break; }
+                    const uint32_t sa = ring + (uint32_t)(s * STAGE), fb = full0 + (uint32_t)(s * 8);
+                    if (rank == 0) mbar_expect_tx_if(first, smem_u32(&sh.full[s]), STAGE * CTAS);
+                    tma_load_2d_if<CTAS>(on, sa, &p.tmX, fb, b * F8_BLOCK, m0);
+                    tma_load_2d_if<CTAS>(on, sa + F8_A_BYTES, &p.tmW, fb, b * F8_BLOCK, f0 + rank * B_ROWS);
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
+                }
+            }
+        } else if (warp == 1 && rank == 0) {
+            const uint32_t on = elect_one(), d_tmem = uniform(tmem_base), empty0 = smem_u32(sh.empty), acc0 = smem_u32(sh.acc_full);
+            // instruction descriptor: fp32 accumulator at bit 4, operand formats at bits 7 / 10, N >> 3 at bit 17, M >> 4 at bit 24
+            const uint32_t idesc = (1u << 4) | p.formats | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TILE_M * CTAS >> 4) << 24);
+            int s = 0, a = 0;
+            uint32_t phase = 0, acc_phase = 1;
+            bool ok = true;
+            for (int tile = group; ok && tile < tiles; tile += groups)
+                for (int b = 0; b < blocks; b++) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(&sh.acc_empty[a], acc_phase, abort_flag)) ||
+                        !__all_sync(0xffffffffu, mbar_wait(&sh.full[s], phase, abort_flag))) { ok = false; break; }
+                    tc_fence_after();
+                    const int steps = min(4, (p.C - b * F8_BLOCK + 31) / 32);
+                    const uint32_t sa = ring + (uint32_t)(s * STAGE);
+                    const uint64_t da = smem_desc_sw128(sa), db = smem_desc_sw128(sa + F8_A_BYTES);
 #pragma unroll
-            for (int q = 0; q < 4; q++)
-                if (q < steps) umma_f8_if(on, d_tmem + (uint32_t)(a * BN), da + (uint64_t)(2 * q), db + (uint64_t)(2 * q), idesc, q > 0 ? 1u : 0u);
-            umma_commit_if(on, empty0 + (uint32_t)(s * 8));
-            umma_commit_if(on, acc0 + (uint32_t)(a * 8));
-            if (++s == stages) { s = 0; phase ^= 1; }
+                    for (int q = 0; q < 4; q++)
+                        if (q < steps) umma_f8_if<CTAS>(on, d_tmem + (uint32_t)(a * BN), da + (uint64_t)(2 * q), db + (uint64_t)(2 * q), idesc, q > 0 ? 1u : 0u);
+                    commit_if<CTAS>(on, empty0 + (uint32_t)(s * 8));
+                    commit_if<CTAS>(on, acc0 + (uint32_t)(a * 8));
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
+                    if (++a == NACC) { a = 0; acc_phase ^= 1; }
+                }
+        } else if (warp == 2) {
+            // scales: eight blocks ahead of their use, without a register (a load just before the block that needs it took as long as
+            // two blocks' MMAs); zeros beyond the operands
+            int i = 0;
+            uint32_t phase = 1;
+            bool ok = true;
+            for (int tile = group; ok && tile < tiles; tile += groups) {
+                int m0, f0;
+                place(tile, &m0, &f0);
+                for (int b = 0; b < blocks; b++) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(&sh.sc_empty[i], phase, abort_flag))) { ok = false; break; }
+                    const float *sx = p.sx + (long long)b * p.ldsx, *sw = p.sw + (long long)b * p.ldsw;
+#pragma unroll
+                    for (int j = 0; j < TILE_M / 32; j++) copy_float(&sh.row_scale[i][32 * j + lane], sx + min(m0 + 32 * j + lane, p.M - 1), m0 + 32 * j + lane < p.M);
+                    if (W_ROWS) {
+#pragma unroll
+                        for (int j = 0; j < BN / 32; j++) copy_float(&sh.col_scale[i][32 * j + lane], sw + min(f0 + 32 * j + lane, p.K - 1), f0 + 32 * j + lane < p.K);
+                    } else if (lane < 2) copy_float(&sh.col_scale[i][lane], sw + min(f0 + lane * COLS, p.K - 1) / 128, true);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.sc_full[i])) : "memory");
+                    if (++i == F8_SCALES) { i = 0; phase ^= 1; }
+                }
+            }
         }
     } else {
-        const int quad = warp & 3, half = warp >= 6 ? 1 : 0;  // (a warp reads the 32 lanes of its number modulo 4)
-        const int m = m0 + quad * 32 + lane, c0 = half * COLS;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int quad = warp & 3, half = warp >> 3;  // (a warp reads the 32 lanes of its number modulo 4)
+        const int c0 = half * COLS, ht = (warp & 3) * 32 + lane;  // first column of the half, thread of it
         const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)c0;
-        const float *sx = p.sx + min(m, p.M - 1);
-        // columns of this half lie in one block of 128 rows of w
-        const float *sw = W_ROWS ? p.sw : p.sw + min(f0 + c0, p.K - 1) / 128;
-        const int ht = (warp - 2) % 4 * 32 + lane;  // thread of the half
-        const int my_col = min(f0 + c0 + ht, p.K - 1);
-        float2 acc[COLS / 2];
+        const uint32_t out0 = ring + F8_RING + (uint32_t)((warp - 4) * 2 * F8_OUT);
+        const uint32_t drained0 = CTAS == 2 ? block_addr(smem_u32(sh.acc_empty), 0) : smem_u32(sh.acc_empty);
+        auto half_sync = [&] {
+            if (half) asm volatile("bar.sync 2, 128;" ::: "memory");
+            else asm volatile("bar.sync 1, 128;" ::: "memory");
+        };
+        int a = 0, parts = 0, i = 0;  // accumulator, output boxes written, scales
+        uint32_t acc_phase = 0, sc_phase = 0;
+        for (int tile = group; tile < tiles; tile += groups) {
+            int m0, f0;
+            place(tile, &m0, &f0);
+            const int m = m0 + quad * 32 + lane, fc = f0 + c0;
+            const float my_bias = p.bias && ht < COLS ? ld_act(p.bias + min(fc + ht, p.K - 1)) : 0.f;
+            float2 acc[COLS / 2];
 #pragma unroll
-        for (int j = 0; j < COLS / 2; j++) acc[j] = make_float2(0.f, 0.f);
-        float next_x = ld_act(sx), next_w = W_ROWS ? (ht < COLS ? ld_act(sw + my_col) : 0.f) : ld_act(sw);
-        for (int b = 0; b < blocks; b++) {
-            const int a = b & 1;
-            const float cur_x = next_x, cur_w = next_w;
-            if (b + 1 < blocks) {
-                next_x = ld_act(sx + (long long)(b + 1) * p.ldsx);
-                if (W_ROWS) { if (ht < COLS) next_w = ld_act(sw + (long long)(b + 1) * p.ldsw + my_col); }
-                else next_w = ld_act(sw + (long long)(b + 1) * p.ldsw);
-            }
-            if (W_ROWS) {
-                if (ht < COLS) col_scale[a][c0 + ht] = cur_w;
-                if (half) asm volatile("bar.sync 2, 128;" ::: "memory");
-                else asm volatile("bar.sync 1, 128;" ::: "memory");
-            }
-            // (after a wait that ran out the warps still go through all steps: the others meet them at the barrier above)
-            if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[a], (uint32_t)(b >> 1) & 1, abort_flag))) continue;
-            tc_fence_after();
-            const float2 s2 = W_ROWS ? make_float2(cur_x, cur_x) : make_float2(cur_x * cur_w, cur_x * cur_w);
+            for (int j = 0; j < COLS / 2; j++) acc[j] = make_float2(0.f, 0.f);
+            for (int b = 0; b < blocks; b++) {
+                // (after a wait that ran out the warps still go through all steps: the others meet them at the barriers below)
+                if (__all_sync(0xffffffffu, mbar_wait(&sh.sc_full[i], sc_phase, abort_flag)) &&
+                    __all_sync(0xffffffffu, mbar_wait(&sh.acc_full[a], acc_phase, abort_flag))) {
+                    const float *cs = sh.col_scale[i];
+                    float f = sh.row_scale[i][quad * 32 + lane];
+                    if (!W_ROWS) f *= cs[half];
+                    const float2 s2 = make_float2(f, f);
+                    tc_fence_after();
+                    uint32_t v[2][32];
+                    tmem_ld32(taddr + (uint32_t)(a * BN), v[0]);
 #pragma unroll
-            for (int j0 = 0; j0 < COLS; j0 += CHUNK) {
-                uint32_t v[CHUNK];
-                tmem_ld32(taddr + (uint32_t)(a * BN + j0), v);
-                tmem_ld_wait();
+                    for (int j0 = 0; j0 < COLS; j0 += 32) {
+                        uint32_t (&w)[32] = v[(j0 / 32) & 1];
+                        tmem_ld_wait32(w);
+                        if (j0 + 32 < COLS) tmem_ld32(taddr + (uint32_t)(a * BN + j0 + 32), v[(j0 / 32 + 1) & 1]);
+                        else {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) arrive_at(drained0 + (uint32_t)(a * 8));
+                        }
 #pragma unroll
-                for (int j = 0; j < CHUNK / 2; j++) {
-                    float2 f = s2;
-                    if (W_ROWS) f = __fmul2_rn(s2, *reinterpret_cast<const float2 *>(&col_scale[a][c0 + j0 + 2 * j]));
-                    acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), f, acc[j0 / 2 + j]);
+                        for (int j = 0; j < 16; j += 2) {
+                            float2 g0 = s2, g1 = s2;
+                            if (W_ROWS) {
+                                const float4 c = *reinterpret_cast<const float4 *>(cs + c0 + j0 + 2 * j);
+                                g0 = __fmul2_rn(s2, make_float2(c.x, c.y));
+                                g1 = __fmul2_rn(s2, make_float2(c.z, c.w));
+                            }
+                            acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1])), g0, acc[j0 / 2 + j]);
+                            acc[j0 / 2 + j + 1] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j + 2]), __uint_as_float(w[2 * j + 3])), g1, acc[j0 / 2 + j + 1]);
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.sc_empty[i]);
                 }
+                if (++a == NACC) { a = 0; acc_phase ^= 1; }
+                if (++i == F8_SCALES) { i = 0; sc_phase ^= 1; }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&acc_empty[a]);
-        }
-        if (!*abort_flag && m < p.M) {
-            const int n = min(COLS, p.K - f0 - c0);
+            // ---- bias, activation, one rounding, output
+            half_sync();  // (all have read the last tile's)
+            if (ht < COLS) sh.bias[c0 + ht] = my_bias;
+            half_sync();
 #pragma unroll
-            for (int j = 0; j < COLS / 2; j++) {
-                if (2 * j >= n) break;
-                if (p.bias) {
-                    acc[j].x += ld_act(p.bias + f0 + c0 + 2 * j);
-                    if (2 * j + 1 < n) acc[j].y += ld_act(p.bias + f0 + c0 + 2 * j + 1);
-                }
-                acc[j].x = act_fn(acc[j].x, p.act);
-                acc[j].y = act_fn(acc[j].y, p.act);
+            for (int j = 0; j < COLS / 2; j++) acc[j] = __fadd2_rn(acc[j], *reinterpret_cast<const float2 *>(&sh.bias[c0 + 2 * j]));
+            if (p.act == ACT_RELU) {
+#pragma unroll
+                for (int j = 0; j < COLS / 2; j++) { acc[j].x = acc[j].x < 0.f ? 0.f : acc[j].x; acc[j].y = acc[j].y < 0.f ? 0.f : acc[j].y; }
+            } else if (p.act == ACT_HSWISH) {
+#pragma unroll
+                for (int j = 0; j < COLS / 2; j++) { acc[j].x = act_fn(acc[j].x, ACT_HSWISH); acc[j].y = act_fn(acc[j].y, ACT_HSWISH); }
             }
-            if (n > 0) store_row<COLS>(p, (long long)m * p.ldy + f0 + c0, reinterpret_cast<const float *>(acc), n);
+            if (*abort_flag) continue;
+            if (p.bulk_y >= min(fc + COLS, p.K)) {
+                // through shared memory in boxes of 32 rows x 64 bytes (64-byte swizzle) and out by the copy unit, which leaves out what lies
+                // beyond the output; two boxes a warp, one being filled while the other is read
+                const bool rows_in = m0 + quad * 32 < p.M;
+                const uint32_t line = (uint32_t)lane * 64, swz = ((uint32_t)lane >> 1) & 3;
+                auto box = [&](const uint4 (&q)[4], int col) {
+                    if (fc + col >= p.K || !rows_in) return;
+                    const uint32_t buf = out0 + (uint32_t)(parts & 1) * F8_OUT;
+                    if (lane == 0 && parts >= 2) bulk_wait_read<1>();
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 4; j++) sts128(buf + line + (((uint32_t)j ^ swz) << 4), q[j]);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&p.tmY, buf, fc + col, m0 + quad * 32);
+                        bulk_commit();
+                    }
+                    parts++;
+                };
+                if (p.y_bf16) {
+#pragma unroll
+                    for (int col = 0; col < COLS; col += 32) {
+                        uint4 q[4];
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&q[j]);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) h[i] = __float22bfloat162_rn(acc[col / 2 + 4 * j + i]);
+                        }
+                        box(q, col);
+                    }
+                } else {
+#pragma unroll
+                    for (int col = 0; col < COLS; col += 16) {
+                        uint4 q[4];
+#pragma unroll
+                        for (int j = 0; j < 4; j++)
+                            q[j] = make_uint4(__float_as_uint(acc[col / 2 + 2 * j].x), __float_as_uint(acc[col / 2 + 2 * j].y), __float_as_uint(acc[col / 2 + 2 * j + 1].x),
+                                              __float_as_uint(acc[col / 2 + 2 * j + 1].y));
+                        box(q, col);
+                    }
+                }
+            } else if (m < p.M) store_row<COLS>(p, (long long)m * p.ldy + fc, reinterpret_cast<const float *>(acc), min(COLS, p.K - fc));
         }
+        if (lane == 0) bulk_wait_all();
     }
     tc_fence_before();
     __syncthreads();
-    if (abort_s) {  // a wait ran out: report, let copies in flight land, then release the tensor memory
+    if (sh.abort) {  // a wait ran out: report, let copies in flight land, then release the tensor memory
         if (threadIdx.x == 0) atomicExch(p.status, 1);
         const unsigned long long t0 = global_ns();
         while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
         __syncthreads();
     }
-    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, 2 * BN); }
+    if (CTAS == 2) pair_sync();  // (the other block's MMAs read this one's shared memory, its warps signal this one's barriers)
+    if (warp == 1) { tc_fence_after(); f8_tmem_dealloc<CTAS>(tmem_base, 512); }
 }
 
 DeviceBits g_set[4];
 
-template <int BN, bool W_ROWS> cudaError_t launch_tiles(F8Params &p, const LinearF8Args &a, DeviceBits &done, cudaStream_t st) {
-    constexpr int STAGE = F8_A_BYTES + BN * F8_BLOCK, STAGES = std::min(192 * 1024 / STAGE, TC_MAX_STAGES);
+template <int CTAS, int BN, bool W_ROWS> cudaError_t launch_tiles(F8Params &p, const LinearF8Args &a, DeviceBits &done, cudaStream_t st) {
+    constexpr int SMEM = F8_RING + F8_SUM_WARPS * 2 * F8_OUT + F8_SCALES * (TILE_M + (W_ROWS ? BN : 4)) * 4 + BN * 4 + 512;
+    static_assert(SMEM <= 227 * 1024, "shared memory");
     if (!tc_encode_bytes(&p.tmX, a.x, (uint64_t)a.C, (uint64_t)a.M, (uint64_t)a.ldx, TILE_M) ||
-        !tc_encode_bytes(&p.tmW, a.w, (uint64_t)a.C, (uint64_t)a.K, (uint64_t)a.ldw, BN))
+        !tc_encode_bytes(&p.tmW, a.w, (uint64_t)a.C, (uint64_t)a.K, (uint64_t)a.ldw, BN / CTAS))
         return cudaErrorInvalidValue;
-    p.m_tiles = (a.M + TILE_M - 1) / TILE_M;
+    p.m_tiles = (a.M + TILE_M * CTAS - 1) / (TILE_M * CTAS);
     p.n_tiles = (a.K + BN - 1) / BN;
-    cudaError_t e = smem_limit_once(linear_f8_kernel<BN, W_ROWS>, STAGES * STAGE + 1024, done);
+    cudaError_t e = smem_limit_once(linear_f8_kernel<CTAS, BN, W_ROWS>, SMEM, done);
     if (e != cudaSuccess) return e;
-    return launch_pdl(linear_f8_kernel<BN, W_ROWS>, dim3((unsigned)(p.m_tiles * p.n_tiles)), dim3(F8_THREADS), STAGES * STAGE + 1024, st, 1, p, STAGES);
+    const long long groups = std::min<long long>((long long)p.m_tiles * p.n_tiles, sm_count() / CTAS);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(groups * CTAS));
+    cfg.blockDim = dim3(F8_THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CTAS; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, linear_f8_kernel<CTAS, BN, W_ROWS>, p);
 }
 
 }  // namespace
@@ -234,11 +389,14 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
     p.ldsx = a.ldsx; p.ldsw = a.ldsw; p.ldy = a.ldy;
     p.M = a.M; p.K = a.K; p.C = a.C; p.blocks = (a.C + F8_BLOCK - 1) / F8_BLOCK;
     p.act = a.act; p.y_bf16 = a.y_bf16;
-    p.vec_y = ((reinterpret_cast<uintptr_t>(a.y) | (size_t)a.ldy * (a.y_bf16 ? 2 : 4)) & 15) == 0;
+    const size_t pitch = (size_t)a.ldy * (a.y_bf16 ? 2 : 4);
+    const int unit = a.y_bf16 ? 8 : 4;  // elements of 16 bytes
+    if (((reinterpret_cast<uintptr_t>(a.y) | pitch) & 15) == 0 && tc_encode_output(&p.tmY, a.y, (uint64_t)a.K, (uint64_t)a.M, pitch, a.y_bf16, 4 * unit, 32))
+        p.bulk_y = a.K / unit * unit;
     p.formats = ((uint32_t)(a.x_e5m2 ? 1 : 0) << 7) | ((uint32_t)(a.w_e5m2 ? 1 : 0) << 10);
-    const bool wide = a.K > 128 && (long long)((a.M + 127) / 128) * ((a.K + 255) / 256) >= sm_count();
-    if (a.w_rows) return wide ? launch_tiles<256, true>(p, a, g_set[0], st) : launch_tiles<128, true>(p, a, g_set[1], st);
-    return wide ? launch_tiles<256, false>(p, a, g_set[2], st) : launch_tiles<128, false>(p, a, g_set[3], st);
+    const bool pairs = (long long)((a.M + 255) / 256) * ((a.K + 255) / 256) * 2 >= sm_count();
+    if (a.w_rows) return pairs ? launch_tiles<2, 256, true>(p, a, g_set[0], st) : launch_tiles<1, 128, true>(p, a, g_set[1], st);
+    return pairs ? launch_tiles<2, 256, false>(p, a, g_set[2], st) : launch_tiles<1, 128, false>(p, a, g_set[3], st);
 }
 
 }  // namespace sgs
