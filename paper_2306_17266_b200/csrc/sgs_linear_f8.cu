@@ -16,7 +16,7 @@ constexpr int F8_BLOCK = 128;                       // reduction steps of a scal
 constexpr int F8_A_BYTES = TILE_M * F8_BLOCK;
 constexpr int F8_SUM_WARPS = 8, F8_THREADS = 128 + 32 * F8_SUM_WARPS;
 constexpr int F8_RING = 160 * 1024;                 // operand stages
-constexpr int F8_SCALES = 8;                        // blocks whose scales are in shared memory or on their way
+constexpr int F8_AHEAD = 4;                         // blocks whose scales travel together; two such sets are in shared memory or on their way
 constexpr int F8_OUT = 2048;                        // an output box of a warp: 32 rows x 64 bytes
 
 struct F8Params {
@@ -79,7 +79,7 @@ __device__ __forceinline__ uint32_t block_addr(uint32_t saddr, uint32_t rank) {
 // Arrival at a barrier of either block, behind tensor-memory loads alone.  (A release at cluster scope waits for all of the thread's
 // memory operations: 1000 to 1700 clocks here, three times a block's MMAs.)
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory"); }
-__device__ __forceinline__ void pair_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pair_sync() { asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory"); }
 template <int CTAS> __device__ __forceinline__ void f8_tmem_alloc(uint32_t *dst, uint32_t cols) {
     if (CTAS == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(cols) : "memory");
@@ -92,6 +92,20 @@ template <int CTAS> __device__ __forceinline__ void f8_tmem_dealloc(uint32_t add
 }
 __device__ __forceinline__ void copy_float(float *dst, const float *src, bool in) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+// Bounded wait of a converged warp, as mbar_wait but in few instructions and without a jump where the phase is complete: the warps that
+// add up wait twice in some 300 instructions.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    unsigned long long t0 = 0;
+#pragma unroll 1
+    for (uint32_t n = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); n++) {
+        if (n & 255) continue;
+        const unsigned long long t = global_ns();
+        if (!t0) t0 = t;
+        if (__any_sync(0xffffffffu, *abort_flag || t - t0 > WAIT_LIMIT_NS)) { *abort_flag = 1; return false; }
+    }
+    return true;
 }
 // Waits for this warp's tensor-memory loads; the values named are the ones that they bring.
 __device__ __forceinline__ void tmem_ld_wait32(uint32_t (&v)[32]) {
@@ -120,9 +134,10 @@ template <int CTAS, int BN, bool W_ROWS>
 __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_constant__ F8Params p) {
     constexpr int B_ROWS = BN / CTAS, STAGE = F8_A_BYTES + B_ROWS * F8_BLOCK, STAGES = F8_RING / STAGE, NACC = 512 / BN, COLS = BN / 2;
     struct Shared {
-        alignas(16) float row_scale[F8_SCALES][TILE_M], col_scale[F8_SCALES][W_ROWS ? BN : 4];  // (not W_ROWS: one for each half of the columns)
+        alignas(16) float row_scale[2][TILE_M][F8_AHEAD];                                   // a thread reads its row's of a set at once
+        alignas(16) float col_scale[2][W_ROWS ? F8_AHEAD : 2][W_ROWS ? BN : F8_AHEAD];       // W_ROWS: [block][column], else [half of the columns][block]
         alignas(16) float bias[BN];
-        alignas(8) uint64_t full[STAGES], empty[STAGES], acc_full[NACC], acc_empty[NACC], sc_full[F8_SCALES], sc_empty[F8_SCALES];
+        alignas(8) uint64_t full[STAGES], empty[STAGES], acc_full[NACC], acc_empty[NACC], sc_full[2], sc_empty[2];
         uint32_t tmem_base;
         int abort;
     };
@@ -134,7 +149,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; s++) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
         for (int i = 0; i < NACC; i++) { mbar_init(&sh.acc_full[i], 1); mbar_init(&sh.acc_empty[i], F8_SUM_WARPS * CTAS); }
-        for (int i = 0; i < F8_SCALES; i++) { mbar_init(&sh.sc_full[i], 32); mbar_init(&sh.sc_empty[i], F8_SUM_WARPS); }
+        for (int i = 0; i < 2; i++) { mbar_init(&sh.sc_full[i], 32); mbar_init(&sh.sc_empty[i], F8_SUM_WARPS); }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -166,7 +181,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                 int m0, f0;
                 place(tile, &m0, &f0);
                 for (int b = 0; b < blocks; b++) {
-                    if (!__all_sync(0xffffffffu, mbar_wait(&sh.empty[s], phase, abort_flag))) { ok = false; break; }
+                    if (!warp_wait(&sh.empty[s], phase, abort_flag)) { ok = false; break; }
                     const uint32_t sa = ring + (uint32_t)(s * STAGE), fb = full0 + (uint32_t)(s * 8);
                     if (rank == 0) mbar_expect_tx_if(first, smem_u32(&sh.full[s]), STAGE * CTAS);
                     tma_load_2d_if<CTAS>(on, sa, &p.tmX, fb, b * F8_BLOCK, m0);
@@ -183,8 +198,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             bool ok = true;
             for (int tile = group; ok && tile < tiles; tile += groups)
                 for (int b = 0; b < blocks; b++) {
-                    if (!__all_sync(0xffffffffu, mbar_wait(&sh.acc_empty[a], acc_phase, abort_flag)) ||
-                        !__all_sync(0xffffffffu, mbar_wait(&sh.full[s], phase, abort_flag))) { ok = false; break; }
+                    if (!warp_wait(&sh.acc_empty[a], acc_phase, abort_flag) ||
+                        !warp_wait(&sh.full[s], phase, abort_flag)) { ok = false; break; }
                     tc_fence_after();
                     const int steps = min(4, (p.C - b * F8_BLOCK + 31) / 32);
                     const uint32_t sa = ring + (uint32_t)(s * STAGE);
@@ -198,25 +213,29 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                     if (++a == NACC) { a = 0; acc_phase ^= 1; }
                 }
         } else if (warp == 2) {
-            // scales: eight blocks ahead of their use, without a register (a load just before the block that needs it took as long as
-            // two blocks' MMAs); zeros beyond the operands
+            // scales: two sets of four blocks ahead of their use, without a register (a load just before the block that needs it took as
+            // long as two blocks' MMAs); zeros beyond the operands
             int i = 0;
             uint32_t phase = 1;
             bool ok = true;
             for (int tile = group; ok && tile < tiles; tile += groups) {
                 int m0, f0;
                 place(tile, &m0, &f0);
-                for (int b = 0; b < blocks; b++) {
-                    if (!__all_sync(0xffffffffu, mbar_wait(&sh.sc_empty[i], phase, abort_flag))) { ok = false; break; }
-                    const float *sx = p.sx + (long long)b * p.ldsx, *sw = p.sw + (long long)b * p.ldsw;
+                for (int b0 = 0; b0 < blocks; b0 += F8_AHEAD) {
+                    if (!warp_wait(&sh.sc_empty[i], phase, abort_flag)) { ok = false; break; }
 #pragma unroll
-                    for (int j = 0; j < TILE_M / 32; j++) copy_float(&sh.row_scale[i][32 * j + lane], sx + min(m0 + 32 * j + lane, p.M - 1), m0 + 32 * j + lane < p.M);
-                    if (W_ROWS) {
+                    for (int k = 0; k < F8_AHEAD; k++) {
+                        if (b0 + k >= blocks) break;
+                        const float *sx = p.sx + (long long)(b0 + k) * p.ldsx, *sw = p.sw + (long long)(b0 + k) * p.ldsw;
 #pragma unroll
-                        for (int j = 0; j < BN / 32; j++) copy_float(&sh.col_scale[i][32 * j + lane], sw + min(f0 + 32 * j + lane, p.K - 1), f0 + 32 * j + lane < p.K);
-                    } else if (lane < 2) copy_float(&sh.col_scale[i][lane], sw + min(f0 + lane * COLS, p.K - 1) / 128, true);
+                        for (int j = 0; j < TILE_M; j += 32) copy_float(&sh.row_scale[i][j + lane][k], sx + min(m0 + j + lane, p.M - 1), m0 + j + lane < p.M);
+                        if (W_ROWS) {
+#pragma unroll
+                            for (int j = 0; j < BN; j += 32) copy_float(&sh.col_scale[i][W_ROWS ? k : 0][j + lane], sw + min(f0 + j + lane, p.K - 1), f0 + j + lane < p.K);
+                        } else if (lane < 2) copy_float(&sh.col_scale[i][lane][W_ROWS ? 0 : k], sw + min(f0 + lane * COLS, p.K - 1) / 128, true);
+                    }
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.sc_full[i])) : "memory");
-                    if (++i == F8_SCALES) { i = 0; phase ^= 1; }
+                    if ((i ^= 1) == 0) phase ^= 1;
                 }
             }
         }
@@ -241,13 +260,25 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             float2 acc[COLS / 2];
 #pragma unroll
             for (int j = 0; j < COLS / 2; j++) acc[j] = make_float2(0.f, 0.f);
+            // (after a wait that ran out the warps still go through all steps: the others meet them at the barriers below)
+            bool ok = true;
+            float rs[F8_AHEAD];
             for (int b = 0; b < blocks; b++) {
-                // (after a wait that ran out the warps still go through all steps: the others meet them at the barriers below)
-                if (__all_sync(0xffffffffu, mbar_wait(&sh.sc_full[i], sc_phase, abort_flag)) &&
-                    __all_sync(0xffffffffu, mbar_wait(&sh.acc_full[a], acc_phase, abort_flag))) {
-                    const float *cs = sh.col_scale[i];
-                    float f = sh.row_scale[i][quad * 32 + lane];
-                    if (!W_ROWS) f *= cs[half];
+                const int k = b % F8_AHEAD;
+                if (k == 0) {
+                    ok = warp_wait(&sh.sc_full[i], sc_phase, abort_flag);
+                    const float4 x4 = *reinterpret_cast<const float4 *>(sh.row_scale[i][quad * 32 + lane]);
+                    rs[0] = x4.x; rs[1] = x4.y; rs[2] = x4.z; rs[3] = x4.w;
+                    if (!W_ROWS) {
+                        const float4 w4 = *reinterpret_cast<const float4 *>(sh.col_scale[i][half]);
+                        rs[0] *= w4.x; rs[1] *= w4.y; rs[2] *= w4.z; rs[3] *= w4.w;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.sc_empty[i]);
+                    }
+                }
+                if (warp_wait(&sh.acc_full[a], acc_phase, abort_flag) && ok) {
+                    const float *cs = sh.col_scale[i][W_ROWS ? k : 0] + c0;
+                    const float f = k & 2 ? (k & 1 ? rs[3] : rs[2]) : (k & 1 ? rs[1] : rs[0]);
                     const float2 s2 = make_float2(f, f);
                     tc_fence_after();
                     uint32_t v[2][32];
@@ -266,7 +297,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                         for (int j = 0; j < 16; j += 2) {
                             float2 g0 = s2, g1 = s2;
                             if (W_ROWS) {
-                                const float4 c = *reinterpret_cast<const float4 *>(cs + c0 + j0 + 2 * j);
+                                const float4 c = *reinterpret_cast<const float4 *>(cs + j0 + 2 * j);
                                 g0 = __fmul2_rn(s2, make_float2(c.x, c.y));
                                 g1 = __fmul2_rn(s2, make_float2(c.z, c.w));
                             }
@@ -274,11 +305,15 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                             acc[j0 / 2 + j + 1] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j + 2]), __uint_as_float(w[2 * j + 3])), g1, acc[j0 / 2 + j + 1]);
                         }
                     }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.sc_empty[i]);
                 }
                 if (++a == NACC) { a = 0; acc_phase ^= 1; }
-                if (++i == F8_SCALES) { i = 0; sc_phase ^= 1; }
+                if (k == F8_AHEAD - 1 || b == blocks - 1) {
+                    if (W_ROWS) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.sc_empty[i]);
+                    }
+                    if ((i ^= 1) == 0) sc_phase ^= 1;
+                }
             }
             // ---- bias, activation, one rounding, output
             half_sync();  // (all have read the last tile's)
@@ -353,10 +388,216 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
     if (warp == 1) { tc_fence_after(); f8_tmem_dealloc<CTAS>(tmem_base, 512); }
 }
 
-DeviceBits g_set[4];
+// Few rows of x: the rows of w take the lanes (128 a block), up to N rows of x the columns, and the blocks of a cluster share the
+// reduction, whose parts meet in distributed shared memory, in the order of c.  What bounds such a call is w's bytes: 16 KB of them a
+// stage, two thread blocks an SM.  Warp 0 loads, 1 issues, 2 brings the scales, warps 4..7 add up, a quadrant of the lanes each.
+constexpr int F8_SPLIT_THREADS = 256, F8_SPLIT_RING = 96 * 1024;
+struct F8Split {
+    int parts, part_blocks;  // blocks of a cluster; blocks of the reduction that each of them takes (the last may have fewer)
+};
+template <int N, bool W_ROWS>
+__global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_split_kernel(const __grid_constant__ F8Params p, const F8Split q) {
+    constexpr int STAGE = F8_A_BYTES + N * F8_BLOCK, STAGES = F8_SPLIT_RING / STAGE, NACC = N <= 32 ? 8 : 256 / N;
+    struct Shared {
+        alignas(16) float w_scale[2][W_ROWS ? TILE_M : 1][F8_AHEAD];
+        alignas(16) float x_scale[2][F8_AHEAD][N];
+        alignas(8) uint64_t full[STAGES], empty[STAGES], acc_full[NACC], acc_empty[NACC], sc_full[2], sc_empty[2];
+        uint32_t tmem_base;
+        int abort;
+    };
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Shared &sh = *reinterpret_cast<Shared *>(smem + F8_SPLIT_RING);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    volatile int *abort_flag = &sh.abort;
+    const int f0 = (int)blockIdx.x * TILE_M, n0 = (int)blockIdx.y * N, part = (int)blockIdx.z;
+    const int b_first = part * q.part_blocks, blocks = min(q.part_blocks, p.blocks - b_first);  // (1 at least)
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; s++) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int i = 0; i < NACC; i++) { mbar_init(&sh.acc_full[i], 1); mbar_init(&sh.acc_empty[i], 4); }
+        for (int i = 0; i < 2; i++) { mbar_init(&sh.sc_full[i], 32); mbar_init(&sh.sc_empty[i], 4); }
+        sh.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(&sh.tmem_base, NACC * N);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = sh.tmem_base;
+    pdl_launch_dependents();
+    pdl_wait();
+    const uint32_t ring = smem_u32(smem);
+    float acc[N];
+    if (warp == 0) {
+        const uint32_t on = elect_one(), full0 = smem_u32(sh.full);
+        int s = 0;
+        uint32_t phase = 1;
+        for (int b = 0; b < blocks; b++) {
+            if (!warp_wait(&sh.empty[s], phase, abort_flag)) break;
+            const uint32_t sa = ring + (uint32_t)(s * STAGE), fb = full0 + (uint32_t)(s * 8);
+            mbar_expect_tx_if(on, fb, STAGE);
+            tma_load_2d_if<1>(on, sa, &p.tmW, fb, (b_first + b) * F8_BLOCK, f0);
+            tma_load_2d_if<1>(on, sa + F8_A_BYTES, &p.tmX, fb, (b_first + b) * F8_BLOCK, n0);
+            if (++s == STAGES) { s = 0; phase ^= 1; }
+        }
+    } else if (warp == 1) {
+        const uint32_t on = elect_one(), d_tmem = uniform(tmem_base), empty0 = smem_u32(sh.empty), acc0 = smem_u32(sh.acc_full);
+        const int n_mma = min(N, (p.M - n0 + 15) & ~15);
+        const uint32_t idesc = (1u << 4) | p.formats | ((uint32_t)(n_mma >> 3) << 17) | ((uint32_t)(TILE_M >> 4) << 24);
+        int s = 0, a = 0;
+        uint32_t phase = 0, acc_phase = 1;
+        for (int b = 0; b < blocks; b++) {
+            if (!warp_wait(&sh.acc_empty[a], acc_phase, abort_flag) || !warp_wait(&sh.full[s], phase, abort_flag)) break;
+            tc_fence_after();
+            const int steps = min(4, (p.C - (b_first + b) * F8_BLOCK + 31) / 32);
+            const uint32_t sa = ring + (uint32_t)(s * STAGE);
+            const uint64_t da = smem_desc_sw128(sa), db = smem_desc_sw128(sa + F8_A_BYTES);
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (k < steps) umma_f8_if<1>(on, d_tmem + (uint32_t)(a * N), da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc, k > 0 ? 1u : 0u);
+            umma_commit_if(on, empty0 + (uint32_t)(s * 8));
+            umma_commit_if(on, acc0 + (uint32_t)(a * 8));
+            if (++s == STAGES) { s = 0; phase ^= 1; }
+            if (++a == NACC) { a = 0; acc_phase ^= 1; }
+        }
+    } else if (warp == 2) {
+        int i = 0;
+        uint32_t phase = 1;
+        for (int b0 = 0; b0 < blocks; b0 += F8_AHEAD) {
+            if (!warp_wait(&sh.sc_empty[i], phase, abort_flag)) break;
+#pragma unroll
+            for (int k = 0; k < F8_AHEAD; k++) {
+                if (b0 + k >= blocks) break;
+                const float *sx = p.sx + (long long)(b_first + b0 + k) * p.ldsx, *sw = p.sw + (long long)(b_first + b0 + k) * p.ldsw;
+#pragma unroll
+                for (int j = 0; j < N; j += 32)
+                    if (N >= 32 || lane < N) copy_float(&sh.x_scale[i][k][j + lane], sx + min(n0 + j + lane, p.M - 1), n0 + j + lane < p.M);
+                if (W_ROWS) {
+#pragma unroll
+                    for (int j = 0; j < TILE_M; j += 32) copy_float(&sh.w_scale[i][W_ROWS ? j + lane : 0][k], sw + min(f0 + j + lane, p.K - 1), f0 + j + lane < p.K);
+                } else if (lane == 0) copy_float(&sh.w_scale[i][0][k], sw + blockIdx.x, true);
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.sc_full[i])) : "memory");
+            if ((i ^= 1) == 0) phase ^= 1;
+        }
+    } else if (warp >= 4) {
+        const int quad = warp & 3, l = quad * 32 + lane;
+        const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16);
+#pragma unroll
+        for (int j = 0; j < N; j++) acc[j] = 0.f;
+        int a = 0, i = 0;
+        uint32_t acc_phase = 0, sc_phase = 0;
+        bool ok = true;
+        float4 w4;
+        for (int b = 0; b < blocks; b++) {
+            const int k = b % F8_AHEAD;
+            if (k == 0) {
+                ok = ok && warp_wait(&sh.sc_full[i], sc_phase, abort_flag);
+                w4 = *reinterpret_cast<const float4 *>(sh.w_scale[i][W_ROWS ? l : 0]);
+            }
+            if (ok && (ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag))) {
+                const float f = k & 2 ? (k & 1 ? w4.w : w4.z) : (k & 1 ? w4.y : w4.x);
+                tc_fence_after();
+#pragma unroll
+                for (int j0 = 0; j0 < N; j0 += 32) {
+                    uint32_t v[32];
+                    if (N >= 32) tmem_ld32(taddr + (uint32_t)(a * N + j0), v);
+                    else {
+                        tmem_ld16(taddr + (uint32_t)(a * N), v);
+#pragma unroll
+                        for (int j = 16; j < 32; j++) v[j] = 0;
+                    }
+                    tmem_ld_wait32(v);
+                    if (j0 + 32 >= N) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.acc_empty[a]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < (N < 32 ? N : 32); j += 4) {
+                        const float4 c = *reinterpret_cast<const float4 *>(&sh.x_scale[i][k][j0 + j]);
+                        acc[j0 + j] += __uint_as_float(v[j]) * (f * c.x);
+                        acc[j0 + j + 1] += __uint_as_float(v[j + 1]) * (f * c.y);
+                        acc[j0 + j + 2] += __uint_as_float(v[j + 2]) * (f * c.z);
+                        acc[j0 + j + 3] += __uint_as_float(v[j + 3]) * (f * c.w);
+                    }
+                }
+            }
+            if (++a == NACC) { a = 0; acc_phase ^= 1; }
+            if (k == F8_AHEAD - 1) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.sc_empty[i]);
+                if ((i ^= 1) == 0) sc_phase ^= 1;
+            }
+        }
+        // the parts' sums: [row of x][lane], in the operand stages (all of this block's MMAs have read theirs)
+        if (q.parts > 1 && ok) {
+            float *sums = reinterpret_cast<float *>(smem) + l;
+#pragma unroll
+            for (int j = 0; j < N; j++) sums[j * TILE_M] = acc[j];
+        }
+    }
+    const bool finisher = warp >= 4;
+    if (q.parts > 1) pair_sync();  // (every thread of every block of the cluster)
+    if (finisher && !*abort_flag) {
+        const int l = (warp & 3) * 32 + lane, f = f0 + l;
+        const float bias = p.bias && f < p.K ? ld_act(p.bias + f) : 0.f;
+        auto put = [&](int n, float v) {
+            if (f >= p.K || n0 + n >= p.M) return;
+            v += bias;
+            if (p.act == ACT_RELU) v = v < 0.f ? 0.f : v;
+            else if (p.act == ACT_HSWISH) v = act_fn(v, ACT_HSWISH);
+            const long long at = (long long)(n0 + n) * p.ldy + f;
+            if (p.y_bf16) static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
+            else static_cast<float *>(p.y)[at] = v;
+        };
+        if (q.parts == 1) {
+#pragma unroll
+            for (int j = 0; j < N; j++) put(j, acc[j]);
+        } else {
+            const int rows = min(N, p.M - n0);
+            for (int n = part; n < rows; n += q.parts) {
+                float v = 0.f;
+                for (int s = 0; s < q.parts; s++) {
+                    float t;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(t) : "r"(block_addr(ring + (uint32_t)(n * TILE_M + l) * 4, (uint32_t)s)) : "memory");
+                    v += t;
+                }
+                put(n, v);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (sh.abort) {  // as above
+        if (threadIdx.x == 0) atomicExch(p.status, 1);
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < 2000000ull) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (q.parts > 1) pair_sync();  // (nobody leaves while another block may still read its sums)
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, NACC * N); }
+}
+
+template <int N, bool W_ROWS> cudaError_t launch_split(F8Params &p, const LinearF8Args &a, DeviceBits &done, cudaStream_t st) {
+    constexpr int SMEM = F8_SPLIT_RING + 2 * F8_AHEAD * ((W_ROWS ? TILE_M : 1) + N) * 4 + 512;
+    if (!tc_encode_bytes(&p.tmX, a.x, (uint64_t)a.C, (uint64_t)a.M, (uint64_t)a.ldx, N) || !tc_encode_bytes(&p.tmW, a.w, (uint64_t)a.C, (uint64_t)a.K, (uint64_t)a.ldw, TILE_M))
+        return cudaErrorInvalidValue;
+    p.formats = ((uint32_t)(a.w_e5m2 ? 1 : 0) << 7) | ((uint32_t)(a.x_e5m2 ? 1 : 0) << 10);
+    cudaError_t e = smem_limit_once(linear_f8_split_kernel<N, W_ROWS>, SMEM, done);
+    if (e != cudaSuccess) return e;
+    const unsigned filters = (unsigned)((a.K + TILE_M - 1) / TILE_M), rows = (unsigned)((a.M + N - 1) / N);
+    F8Split q;
+    q.parts = 1;
+    while (q.parts < 8 && (long long)filters * rows * q.parts < sm_count() && p.blocks >= 4 * q.parts) q.parts *= 2;
+    q.part_blocks = (p.blocks + q.parts - 1) / q.parts;
+    while ((q.parts - 1) * q.part_blocks >= p.blocks) q.parts--;  // (no block without a share; any number makes a cluster)
+    return launch_pdl(linear_f8_split_kernel<N, W_ROWS>, dim3(filters, rows, (unsigned)q.parts), dim3(F8_SPLIT_THREADS), SMEM, st, (unsigned)q.parts, p, q);
+}
+
+DeviceBits g_set[12];
 
 template <int CTAS, int BN, bool W_ROWS> cudaError_t launch_tiles(F8Params &p, const LinearF8Args &a, DeviceBits &done, cudaStream_t st) {
-    constexpr int SMEM = F8_RING + F8_SUM_WARPS * 2 * F8_OUT + F8_SCALES * (TILE_M + (W_ROWS ? BN : 4)) * 4 + BN * 4 + 512;
+    constexpr int SMEM = F8_RING + F8_SUM_WARPS * 2 * F8_OUT + 2 * F8_AHEAD * (TILE_M + (W_ROWS ? BN : 2)) * 4 + BN * 4 + 512;
     static_assert(SMEM <= 227 * 1024, "shared memory");
     if (!tc_encode_bytes(&p.tmX, a.x, (uint64_t)a.C, (uint64_t)a.M, (uint64_t)a.ldx, TILE_M) ||
         !tc_encode_bytes(&p.tmW, a.w, (uint64_t)a.C, (uint64_t)a.K, (uint64_t)a.ldw, BN / CTAS))
@@ -394,6 +635,11 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
     if (((reinterpret_cast<uintptr_t>(a.y) | pitch) & 15) == 0 && tc_encode_output(&p.tmY, a.y, (uint64_t)a.K, (uint64_t)a.M, pitch, a.y_bf16, 4 * unit, 32))
         p.bulk_y = a.K / unit * unit;
     p.formats = ((uint32_t)(a.x_e5m2 ? 1 : 0) << 7) | ((uint32_t)(a.w_e5m2 ? 1 : 0) << 10);
+    const long long tiles = (long long)((a.M + 127) / 128) * ((a.K + 127) / 128);
+    if (a.M <= 16) return a.w_rows ? launch_split<16, true>(p, a, g_set[4], st) : launch_split<16, false>(p, a, g_set[5], st);
+    if (a.M <= 32) return a.w_rows ? launch_split<32, true>(p, a, g_set[6], st) : launch_split<32, false>(p, a, g_set[7], st);
+    if (a.M <= 64) return a.w_rows ? launch_split<64, true>(p, a, g_set[8], st) : launch_split<64, false>(p, a, g_set[9], st);
+    if (tiles < sm_count()) return a.w_rows ? launch_split<128, true>(p, a, g_set[10], st) : launch_split<128, false>(p, a, g_set[11], st);
     const bool pairs = (long long)((a.M + 255) / 256) * ((a.K + 255) / 256) * 2 >= sm_count();
     if (a.w_rows) return pairs ? launch_tiles<2, 256, true>(p, a, g_set[0], st) : launch_tiles<1, 128, true>(p, a, g_set[1], st);
     return pairs ? launch_tiles<2, 256, false>(p, a, g_set[2], st) : launch_tiles<1, 128, false>(p, a, g_set[3], st);
