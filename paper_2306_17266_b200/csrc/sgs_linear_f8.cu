@@ -260,13 +260,18 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             float2 acc[COLS / 2];
 #pragma unroll
             for (int j = 0; j < COLS / 2; j++) acc[j] = make_float2(0.f, 0.f);
-            // (after a wait that ran out the warps still go through all steps: the others meet them at the barriers below)
-            bool ok = true;
+            // The tensor memory is read a chunk of 32 columns ahead, over the end of a block too: while the last chunk is added up, the
+            // next block's first one is on its way.  (After a wait that ran out the warps leave the loop and meet the others at the
+            // barriers below.)
+            uint32_t v[2][32];
             float rs[F8_AHEAD];
-            for (int b = 0; b < blocks; b++) {
+            bool ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag);
+            tc_fence_after();
+            if (ok) tmem_ld32(taddr + (uint32_t)(a * BN), v[0]);
+            for (int b = 0; ok && b < blocks; b++) {
                 const int k = b % F8_AHEAD;
                 if (k == 0) {
-                    ok = warp_wait(&sh.sc_full[i], sc_phase, abort_flag);
+                    if (!(ok = warp_wait(&sh.sc_full[i], sc_phase, abort_flag))) break;
                     const float4 x4 = *reinterpret_cast<const float4 *>(sh.row_scale[i][quad * 32 + lane]);
                     rs[0] = x4.x; rs[1] = x4.y; rs[2] = x4.z; rs[3] = x4.w;
                     if (!W_ROWS) {
@@ -276,37 +281,38 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                         if (lane == 0) mbar_arrive(&sh.sc_empty[i]);
                     }
                 }
-                if (warp_wait(&sh.acc_full[a], acc_phase, abort_flag) && ok) {
-                    const float *cs = sh.col_scale[i][W_ROWS ? k : 0] + c0;
-                    const float f = k & 2 ? (k & 1 ? rs[3] : rs[2]) : (k & 1 ? rs[1] : rs[0]);
-                    const float2 s2 = make_float2(f, f);
-                    tc_fence_after();
-                    uint32_t v[2][32];
-                    tmem_ld32(taddr + (uint32_t)(a * BN), v[0]);
+                const float *cs = sh.col_scale[i][W_ROWS ? k : 0] + c0;
+                const float f = rs[0];
+                rs[0] = rs[1]; rs[1] = rs[2]; rs[2] = rs[3];
+                const float2 s2 = make_float2(f, f);
 #pragma unroll
-                    for (int j0 = 0; j0 < COLS; j0 += 32) {
-                        uint32_t (&w)[32] = v[(j0 / 32) & 1];
-                        tmem_ld_wait32(w);
-                        if (j0 + 32 < COLS) tmem_ld32(taddr + (uint32_t)(a * BN + j0 + 32), v[(j0 / 32 + 1) & 1]);
-                        else {
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) arrive_at(drained0 + (uint32_t)(a * 8));
-                        }
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            float2 g0 = s2, g1 = s2;
-                            if (W_ROWS) {
-                                const float4 c = *reinterpret_cast<const float4 *>(cs + j0 + 2 * j);
-                                g0 = __fmul2_rn(s2, make_float2(c.x, c.y));
-                                g1 = __fmul2_rn(s2, make_float2(c.z, c.w));
-                            }
-                            acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1])), g0, acc[j0 / 2 + j]);
-                            acc[j0 / 2 + j + 1] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j + 2]), __uint_as_float(w[2 * j + 3])), g1, acc[j0 / 2 + j + 1]);
+                for (int j0 = 0; j0 < COLS; j0 += 32) {
+                    uint32_t (&w)[32] = v[(j0 / 32) & 1], (&next)[32] = v[(j0 / 32 + 1) & 1];
+                    tmem_ld_wait32(w);
+                    if (j0 + 32 < COLS) tmem_ld32(taddr + (uint32_t)(a * BN + j0 + 32), next);
+                    else {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_at(drained0 + (uint32_t)(a * 8));
+                        if (++a == NACC) { a = 0; acc_phase ^= 1; }
+                        if (b + 1 < blocks) {
+                            ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag);
+                            tc_fence_after();
+                            tmem_ld32(taddr + (uint32_t)(a * BN), next);
                         }
                     }
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) {
+                        float2 g0 = s2, g1 = s2;
+                        if (W_ROWS) {
+                            const float4 c = *reinterpret_cast<const float4 *>(cs + j0 + 2 * j);
+                            g0 = __fmul2_rn(s2, make_float2(c.x, c.y));
+                            g1 = __fmul2_rn(s2, make_float2(c.z, c.w));
+                        }
+                        acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1])), g0, acc[j0 / 2 + j]);
+                        acc[j0 / 2 + j + 1] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j + 2]), __uint_as_float(w[2 * j + 3])), g1, acc[j0 / 2 + j + 1]);
+                    }
                 }
-                if (++a == NACC) { a = 0; acc_phase ^= 1; }
                 if (k == F8_AHEAD - 1 || b == blocks - 1) {
                     if (W_ROWS) {
                         __syncwarp();
@@ -426,7 +432,7 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
     pdl_launch_dependents();
     pdl_wait();
     const uint32_t ring = smem_u32(smem);
-    float acc[N];
+    float2 acc[N / 2];
     if (warp == 0) {
         const uint32_t on = elect_one(), full0 = smem_u32(sh.full);
         int s = 0;
@@ -483,7 +489,7 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
         const int quad = warp & 3, l = quad * 32 + lane;
         const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16);
 #pragma unroll
-        for (int j = 0; j < N; j++) acc[j] = 0.f;
+        for (int j = 0; j < N / 2; j++) acc[j] = make_float2(0.f, 0.f);
         int a = 0, i = 0;
         uint32_t acc_phase = 0, sc_phase = 0;
         bool ok = true;
@@ -496,6 +502,7 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
             }
             if (ok && (ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag))) {
                 const float f = k & 2 ? (k & 1 ? w4.w : w4.z) : (k & 1 ? w4.y : w4.x);
+                const float2 f2 = make_float2(f, f);
                 tc_fence_after();
 #pragma unroll
                 for (int j0 = 0; j0 < N; j0 += 32) {
@@ -515,10 +522,9 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
 #pragma unroll
                     for (int j = 0; j < (N < 32 ? N : 32); j += 4) {
                         const float4 c = *reinterpret_cast<const float4 *>(&sh.x_scale[i][k][j0 + j]);
-                        acc[j0 + j] += __uint_as_float(v[j]) * (f * c.x);
-                        acc[j0 + j + 1] += __uint_as_float(v[j + 1]) * (f * c.y);
-                        acc[j0 + j + 2] += __uint_as_float(v[j + 2]) * (f * c.z);
-                        acc[j0 + j + 3] += __uint_as_float(v[j + 3]) * (f * c.w);
+                        float2 &a0 = acc[(j0 + j) / 2], &a1 = acc[(j0 + j) / 2 + 1];
+                        a0 = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), __fmul2_rn(f2, make_float2(c.x, c.y)), a0);
+                        a1 = __ffma2_rn(make_float2(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), __fmul2_rn(f2, make_float2(c.z, c.w)), a1);
                     }
                 }
             }
@@ -533,7 +539,7 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
         if (q.parts > 1 && ok) {
             float *sums = reinterpret_cast<float *>(smem) + l;
 #pragma unroll
-            for (int j = 0; j < N; j++) sums[j * TILE_M] = acc[j];
+            for (int j = 0; j < N; j++) sums[j * TILE_M] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
         }
     }
     const bool finisher = warp >= 4;
@@ -552,7 +558,7 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
         };
         if (q.parts == 1) {
 #pragma unroll
-            for (int j = 0; j < N; j++) put(j, acc[j]);
+            for (int j = 0; j < N; j++) put(j, j & 1 ? acc[j / 2].y : acc[j / 2].x);
         } else {
             const int rows = min(N, p.M - n0);
             for (int n = part; n < rows; n += q.parts) {
@@ -594,7 +600,7 @@ template <int N, bool W_ROWS> cudaError_t launch_split(F8Params &p, const Linear
     return launch_pdl(linear_f8_split_kernel<N, W_ROWS>, dim3(filters, rows, (unsigned)q.parts), dim3(F8_SPLIT_THREADS), SMEM, st, (unsigned)q.parts, p, q);
 }
 
-DeviceBits g_set[12];
+DeviceBits g_set[10];
 
 template <int CTAS, int BN, bool W_ROWS> cudaError_t launch_tiles(F8Params &p, const LinearF8Args &a, DeviceBits &done, cudaStream_t st) {
     constexpr int SMEM = F8_RING + F8_SUM_WARPS * 2 * F8_OUT + 2 * F8_AHEAD * (TILE_M + (W_ROWS ? BN : 2)) * 4 + BN * 4 + 512;
@@ -638,8 +644,7 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
     const long long tiles = (long long)((a.M + 127) / 128) * ((a.K + 127) / 128);
     if (a.M <= 16) return a.w_rows ? launch_split<16, true>(p, a, g_set[4], st) : launch_split<16, false>(p, a, g_set[5], st);
     if (a.M <= 32) return a.w_rows ? launch_split<32, true>(p, a, g_set[6], st) : launch_split<32, false>(p, a, g_set[7], st);
-    if (a.M <= 64) return a.w_rows ? launch_split<64, true>(p, a, g_set[8], st) : launch_split<64, false>(p, a, g_set[9], st);
-    if (tiles < sm_count()) return a.w_rows ? launch_split<128, true>(p, a, g_set[10], st) : launch_split<128, false>(p, a, g_set[11], st);
+    if (a.M <= 64 || tiles < sm_count()) return a.w_rows ? launch_split<64, true>(p, a, g_set[8], st) : launch_split<64, false>(p, a, g_set[9], st);
     const bool pairs = (long long)((a.M + 255) / 256) * ((a.K + 255) / 256) * 2 >= sm_count();
     if (a.w_rows) return pairs ? launch_tiles<2, 256, true>(p, a, g_set[0], st) : launch_tiles<1, 128, true>(p, a, g_set[1], st);
     return pairs ? launch_tiles<2, 256, false>(p, a, g_set[2], st) : launch_tiles<1, 128, false>(p, a, g_set[3], st);
