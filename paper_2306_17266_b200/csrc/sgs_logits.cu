@@ -62,6 +62,25 @@ template <typename T> __device__ __forceinline__ Split split_row(const T *row, i
     return s;
 }
 
+// Calls f(vector, its number) for this thread's vectors first + t, first + t + THREADS ...: the next U are on their way while U are taken.
+template <int THREADS, int U, typename F> __device__ __forceinline__ void stream(const uint4 *vec, int first, int last, int t, F f) {
+    uint4 q[U], next[U];
+    int i = first + t;
+#pragma unroll
+    for (int u = 0; u < U; u++)
+        if (i + u * THREADS < last) q[u] = ld_act(vec + i + u * THREADS);
+    for (; i < last; i += U * THREADS) {
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (i + (U + u) * THREADS < last) next[u] = ld_act(vec + i + (U + u) * THREADS);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (i + u * THREADS < last) f(q[u], i + u * THREADS);
+#pragma unroll
+        for (int u = 0; u < U; u++) q[u] = next[u];
+    }
+}
+
 // ---- clusters along z ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -315,20 +334,34 @@ __device__ __forceinline__ float2 join(float2 p, float2 q, float a) {
     const float m = fmaxf(p.x, q.x), b = m == NEG_INF ? 0.f : m;
     return make_float2(m, p.y * pow2((p.x - b) * a) + q.y * pow2((q.x - b) * a));
 }
-template <int THREADS> __device__ __forceinline__ void block_join(float2 &u, float2 &v, float a, float4 *buf) {
+// The same of all values of a warp: largest first, then the sums relative to it.
+__device__ __forceinline__ float2 warp_join(float2 v, float a) {
+    float m = v.x;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        u = join(u, make_float2(__shfl_xor_sync(0xffffffffu, u.x, o), __shfl_xor_sync(0xffffffffu, u.y, o)), a);
-        v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)), a);
-    }
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = make_float4(u.x, u.y, v.x, v.y);
-    __syncthreads();
-    u = v = make_float2(NEG_INF, 0.f);
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float s = v.y * pow2((v.x - (m == NEG_INF ? 0.f : m)) * a);
 #pragma unroll
-    for (int i = 0; i < THREADS / 32; i++) {
-        u = join(u, make_float2(buf[i].x, buf[i].y), a);
-        v = join(v, make_float2(buf[i].z, buf[i].w), a);
-    }
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return make_float2(m, s);
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The largest of a vector's elements, NaN left out.
+__device__ __forceinline__ float vec_most(const uint4 &q, const float *) {
+    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+}
+__device__ __forceinline__ float vec_most(const uint4 &q, const __nv_bfloat16 *) {
+    auto two = [](uint32_t x, uint32_t y) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+        return r;
+    };
+    const uint32_t m = two(two(q.x, q.y), two(q.z, q.w));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
 }
 
 struct DisParams {
@@ -337,166 +370,222 @@ struct DisParams {
     const float *teacher, *row_scale;
     const int *index;
     float *loss, *stat;
-    int V, k, backward, parts;
+    int V, k, backward, parts, table;  // table: places of the table of classes, a power of two
     long long ldz, lddz, ldt;
     float inv_t, temperature, grad_scale;
 };
 
-template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const DisParams p) {
-    constexpr int N = Vec<T>::N, U = 4;
-    __shared__ float4 buf[THREADS / 32];
-    __shared__ float sums[THREADS / 32];
+// A team of TEAM threads takes a row (or a cluster's part of one): a block, or for short rows a warp, four to a block.
+//
+// What costs time besides the bytes is the chain of one row: list, row, two reductions, gradient.  So the list and the row's scale are
+// asked for before the row is streamed and looked at behind it, the loss is summed behind the gradient, and the sums over slots that name
+// the same class are formed by the threads that own the slots while the others write.
+template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) distill_kernel(const DisParams p, const int rows) {
+    constexpr int N = Vec<T>::N, U = 4, TEAMS = BLOCK / TEAM, SLOTS = TEAM == 32 ? 4 : DISTILL_TOP_MAX / TEAM;
+    // a row's slots: (class, probability), class -1: not in use; then, for long lists, a table of the classes named, which tells whether one is
+    // named twice
+    extern __shared__ float2 lists[];
+    __shared__ int twice[TEAMS];
+    __shared__ float4 joined[BLOCK / 32];
+    __shared__ float sums[BLOCK / 32];
     __shared__ __align__(8) float2 mine;
-    __shared__ int at[DISTILL_TOP_MAX];
-    __shared__ float prob[DISTILL_TOP_MAX], zl[DISTILL_TOP_MAX];
-    const int t = threadIdx.x, V = p.V, k = p.k, part = (int)blockIdx.z;
-    const long long r = blockIdx.x;
+    const int t = (int)threadIdx.x % TEAM, team = (int)threadIdx.x / TEAM, V = p.V, k = p.k, part = (int)blockIdx.z;
+    const long long r = (long long)blockIdx.x * TEAMS + team;
     pdl_launch_dependents();
     pdl_wait();
+    if (TEAM == 32 && r >= rows) return;
+    auto sync = [&] {
+        if (TEAM == 32) __syncwarp();
+        else __syncthreads();
+    };
+    float2 *list = lists + team * (k + p.table / 2);
+    int *table = reinterpret_cast<int *>(list + k);
+    if (p.table) {
+        for (int j = t; j < p.table; j += TEAM) table[j] = -1;
+        if (t == 0) twice[team] = 0;
+        sync();
+    }
     const T *row = static_cast<const T *>(p.z) + r * p.ldz;
     const float a = p.inv_t * LOG2E;
     const Split s = split_row(row, V, part, p.parts);
     const uint4 *vec = reinterpret_cast<const uint4 *>(row + s.head);
-
-    // the teacher's list (every block of the row reads it): slots not in use have at = -1
-    float2 teach = make_float2(NEG_INF, 0.f), stud = make_float2(NEG_INF, 0.f);
-    for (int j = t; j < k; j += THREADS) {
-        int i = ld_act(p.index + r * p.ldt + j);
-        const float v = ld_act(p.teacher + r * p.ldt + j);
-        if (i < 0 || i >= V || v == NEG_INF) i = -1;
-        at[j] = i;
-        prob[j] = v;
-        zl[j] = i >= 0 ? to_float(ld_act(row + i)) : 0.f;
-        if (i >= 0) teach = join(teach, make_float2(v == v ? v : NEG_INF, v == v ? 1.f : v), a);
-    }
-    if (!p.backward) {
-        float m = NEG_INF, sum = 0.f;
-        auto add = [&](auto &v) {
-            float most = v[0];
+    int at[SLOTS];
+    float tv[SLOTS], zl[SLOTS];
 #pragma unroll
-            for (int j = 1; j < (int)(sizeof(v) / sizeof(float)); j++) most = fmaxf(most, v[j]);
+    for (int q = 0; q < SLOTS; q++) {
+        const bool in = t + q * TEAM < k;
+        at[q] = in ? ld_act(p.index + r * p.ldt + t + q * TEAM) : -1;
+        tv[q] = in ? ld_act(p.teacher + r * p.ldt + t + q * TEAM) : NEG_INF;
+    }
+    const float row_scale = p.dz && p.row_scale ? ld_act(p.row_scale + r) : 1.f;
+    float2 stud = make_float2(NEG_INF, 0.f), kept = make_float2(NEG_INF, 0.f);
+    if (p.backward) kept = make_float2(ld_act(p.stat + 2 * r), ld_act(p.stat + 2 * r + 1));
+    else {
+        // (two elements an instruction where there is one for that)
+        const float2 a2 = make_float2(a, a);
+        float m = NEG_INF;
+        float2 sum = make_float2(0.f, 0.f);
+        auto raise = [&](float most) {  // the largest of the next elements
             if (most > m) {
-                sum *= pow2((m - most) * a);
+                const float f = pow2((m - most) * a);
+                sum.x *= f; sum.y *= f;
                 m = most;
             }
-            const float b = m == NEG_INF ? 0.f : m;
-#pragma unroll
-            for (int j = 0; j < (int)(sizeof(v) / sizeof(float)); j++) sum += pow2((v[j] - b) * a);
+            return m == NEG_INF ? 0.f : -m;
         };
-        for (int i = s.first + t; i < s.last; i += U * THREADS) {
-            uint4 q[U];
+        stream<TEAM, U>(vec, s.first, s.last, t, [&](const uint4 &q, int) {
+            float v[N];
+            unpack(q, v);
+            const float b = raise(vec_most(q, (const T *)nullptr));
+            const float2 b2 = make_float2(b, b);
 #pragma unroll
-            for (int u = 0; u < U; u++)
-                if (i + u * THREADS < s.last) q[u] = ld_act(vec + i + u * THREADS);
-#pragma unroll
-            for (int u = 0; u < U; u++)
-                if (i + u * THREADS < s.last) {
-                    float v[N];
-                    unpack(q[u], v);
-                    add(v);
-                }
-        }
+            for (int j = 0; j < N; j += 2) {
+                const float2 x = __fmul2_rn(__fadd2_rn(make_float2(v[j], v[j + 1]), b2), a2);
+                sum = __fadd2_rn(sum, make_float2(pow2(x.x), pow2(x.y)));
+            }
+        });
         if (t < s.edges) {
-            float v[1] = {to_float(ld_act(row + s.edge(t)))};
-            add(v);
+            const float v = to_float(ld_act(row + s.edge(t))), b = raise(v == v ? v : NEG_INF);
+            sum.x += pow2((v + b) * a);
         }
-        stud = make_float2(m, sum);
+        stud = make_float2(m, sum.x + sum.y);
     }
-    block_join<THREADS>(stud, teach, a, buf);
+    // the teacher's list (every block of the row reads it)
+    float2 teach = make_float2(NEG_INF, 0.f);
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        if (at[q] < 0 || at[q] >= V || tv[q] == NEG_INF) at[q] = -1;
+        zl[q] = at[q] >= 0 ? to_float(ld_act(row + at[q])) : 0.f;
+        if (at[q] < 0) continue;
+        teach = join(teach, make_float2(tv[q] == tv[q] ? tv[q] : NEG_INF, tv[q] == tv[q] ? 1.f : tv[q]), a);
+        if (p.table)
+            for (int h = at[q] * 40503 & (p.table - 1);; h = (h + 1) & (p.table - 1)) {  // (never full: it has at least twice as many places as slots)
+                const int there = atomicCAS(&table[h], -1, at[q]);
+                if (there == at[q]) twice[team] = 1;
+                if (there == -1 || there == at[q]) break;
+            }
+    }
+    stud = warp_join(stud, a);
+    teach = warp_join(teach, a);
+    if (TEAM > 32) {
+        if ((t & 31) == 0) joined[t >> 5] = make_float4(stud.x, stud.y, teach.x, teach.y);
+        __syncthreads();
+        const float4 j = (t & 31) < TEAM / 32 ? joined[t & 31] : make_float4(NEG_INF, 0.f, NEG_INF, 0.f);
+        stud = warp_join(make_float2(j.x, j.y), a);
+        teach = warp_join(make_float2(j.z, j.w), a);
+    }
     const bool used = !(teach.x == NEG_INF && teach.y == 0.f);  // (a sum of NaN is one: slots are in use)
-    if (p.parts > 1 && !p.backward) {
+    const bool meet = TEAM > 32 && p.parts > 1 && !p.backward;
+    if (meet) {
         if (t == 0) mine = stud;
         cluster_arrive();
         cluster_wait();
-        stud = make_float2(NEG_INF, 0.f);
-        for (int q = 0; q < p.parts; q++) stud = join(stud, peer_ld2(peer_addr(&mine, q)), a);
+        stud = (t & 31) < p.parts ? peer_ld2(peer_addr(&mine, t & 31)) : make_float2(NEG_INF, 0.f);
+        stud = warp_join(stud, a);
         cluster_arrive();  // (nobody leaves before all have read: the wait is at the end)
     }
-    float zmax = stud.x, logsum = logf(stud.y);
-    if (p.backward) {
-        zmax = ld_act(p.stat + 2 * r);
-        logsum = ld_act(p.stat + 2 * r + 1);
-    }
+    const float zmax = p.backward ? kept.x : stud.x, logsum = p.backward ? kept.y : logf(stud.y);
     const float base = zmax == NEG_INF ? 0.f : zmax, off = zmax == NEG_INF ? 0.f : logsum;
     const float tmax = teach.x == NEG_INF ? 0.f : teach.x, tsum = teach.y;
-    if (!p.backward && part == 0) {
-        const float log_tsum = logf(tsum);
-        float loss = 0.f;
-        for (int j = t; j < k; j += THREADS)
-            if (at[j] >= 0) {  // (the thread's own slots: no barrier needed)
-                // T (log p - log q), with differences of logits as they are: masks of the type's lowest value do not overflow
-                const float term = (prob[j] - tmax) - (zl[j] - base) + p.temperature * (off - log_tsum);
-                const float pj = pow2((prob[j] - tmax) * a) / tsum;
-                if (!(pj <= 0.f)) loss += pj * term;
+    const float c = used ? p.grad_scale * p.temperature * row_scale : 0.f, off2 = off * LOG2E;
+    float loss = 0.f;
+    const float log_tsum = logf(tsum);
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        if (t + q * TEAM >= k) continue;
+        const float pj = at[q] >= 0 ? pow2((tv[q] - tmax) * a) / tsum : 0.f;
+        // T (log p - log q), with differences of logits as they are: masks of the type's lowest value do not overflow
+        if (at[q] >= 0 && !(pj <= 0.f)) loss += pj * ((tv[q] - tmax) - (zl[q] - base) + p.temperature * (off - log_tsum));
+        if (p.dz) list[t + q * TEAM] = make_float2(__int_as_float(at[q]), pj);
+    }
+    if (p.dz) {
+        T *out = static_cast<T *>(p.dz) + r * p.lddz;
+        sync();
+        // the named classes of this part: q less the probability of all slots with that class, rounded once, written behind the others
+        const long long e0 = s.head + (long long)s.first * N, e1 = s.head + (long long)s.last * N;
+        float named[SLOTS];
+#pragma unroll
+        for (int q = 0; q < SLOTS; q++) {
+            const int i = at[q];
+            if (!((i >= e0 && i < e1) || (part == 0 && i >= 0 && (i < s.head || i >= s.tail)))) at[q] = -1;
+            named[q] = 0.f;
+            if (at[q] < 0 || c == 0.f) continue;
+            float sum = list[t + q * TEAM].y;
+            if (!p.table || twice[team]) {
+                sum = 0.f;
+                for (int l = 0; l < k; l++) sum += __float_as_int(list[l].x) == i ? list[l].y : 0.f;
             }
+            named[q] = c * (pow2((zl[q] - base) * a - off2) - sum);
+        }
+        const bool same = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+        const float2 a2 = make_float2(a, a), base2 = make_float2(-base, -base), less2 = make_float2(-off2, -off2), c2 = make_float2(c, c);
+        auto store = [&](int i, const float (&v)[N]) {
+            T *dst = out + s.head + (long long)i * N;
+            if (same) *reinterpret_cast<uint4 *>(dst) = pack(v);
+            else {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-        if ((t & 31) == 0) sums[t >> 5] = loss;
-        __syncthreads();
+                for (int j = 0; j < N; j++) from_float(dst + j, v[j]);
+            }
+        };
+        if (c != 0.f)
+            stream<TEAM, U>(vec, s.first, s.last, t, [&](const uint4 &q, int i) {
+                float v[N];
+                unpack(q, v);
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    const float2 x = __ffma2_rn(__fadd2_rn(make_float2(v[j], v[j + 1]), base2), a2, less2);
+                    const float2 g = __fmul2_rn(make_float2(pow2(x.x), pow2(x.y)), c2);
+                    v[j] = g.x; v[j + 1] = g.y;
+                }
+                store(i, v);
+            });
+        else {
+            const float zeros[N] = {};
+            for (int i = s.first + t; i < s.last; i += TEAM) store(i, zeros);
+        }
+        if (t < s.edges) {
+            const long long e = s.edge(t);
+            from_float(out + e, c != 0.f ? c * pow2((to_float(ld_act(row + e)) - base) * a - off2) : 0.f);
+        }
+        sync();
+#pragma unroll
+        for (int q = 0; q < SLOTS; q++)
+            if (at[q] >= 0) from_float(out + at[q], named[q]);
+    }
+    if (!p.backward && part == 0) {
+        loss = warp_sum(loss);
+        if (TEAM > 32) {
+            if ((t & 31) == 0) sums[t >> 5] = loss;
+            __syncthreads();
+            if (t < 32) loss = warp_sum(t < TEAM / 32 ? sums[t] : 0.f);
+        }
         if (t == 0) {
-            loss = 0.f;
-#pragma unroll
-            for (int i = 0; i < THREADS / 32; i++) loss += sums[i];
             p.loss[r] = used ? loss * p.temperature : 0.f;
             if (p.stat) { p.stat[2 * r] = zmax; p.stat[2 * r + 1] = logsum; }
         }
     }
-    if (p.dz) {
-        T *out = static_cast<T *>(p.dz) + r * p.lddz;
-        const float c = used ? p.grad_scale * p.temperature * (p.row_scale ? ld_act(p.row_scale + r) : 1.f) : 0.f;
-        const float off2 = off * LOG2E;
-        const bool same = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-        auto grad = [&](float v) { return c * pow2((v - base) * a - off2); };
-        for (int j = t; j < k; j += THREADS) prob[j] = at[j] >= 0 ? pow2((prob[j] - tmax) * a) / tsum : 0.f;
-        for (int i = s.first + t; i < s.last; i += U * THREADS) {
-            uint4 q[U];
-            if (c != 0.f) {
-#pragma unroll
-                for (int u = 0; u < U; u++)
-                    if (i + u * THREADS < s.last) q[u] = ld_act(vec + i + u * THREADS);
-            }
-#pragma unroll
-            for (int u = 0; u < U; u++)
-                if (i + u * THREADS < s.last) {
-                    float v[N];
-                    if (c != 0.f) {
-                        unpack(q[u], v);
-#pragma unroll
-                        for (int j = 0; j < N; j++) v[j] = grad(v[j]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < N; j++) v[j] = 0.f;
-                    }
-                    T *dst = out + s.head + (long long)(i + u * THREADS) * N;
-                    if (same) *reinterpret_cast<uint4 *>(dst) = pack(v);
-                    else {
-#pragma unroll
-                        for (int j = 0; j < N; j++) from_float(dst + j, v[j]);
-                    }
-                }
-        }
-        if (t < s.edges) {
-            const long long e = s.edge(t);
-            from_float(out + e, c != 0.f ? grad(to_float(ld_act(row + e))) : 0.f);
-        }
-        __syncthreads();
-        // the named classes of this part, a warp a slot: q less the probability of all slots with that class, rounded once
-        const long long e0 = s.head + (long long)s.first * N, e1 = s.head + (long long)s.last * N;
-        for (int j = t >> 5; j < k; j += THREADS / 32) {
-            const int i = at[j];
-            if (i < 0 || c == 0.f || !((i >= e0 && i < e1) || (part == 0 && (i < s.head || i >= s.tail)))) continue;
-            float sum = 0.f;
-            for (int l = t & 31; l < k; l += 32) sum += at[l] == i ? prob[l] : 0.f;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if ((t & 31) == 0) from_float(out + i, c * (pow2((zl[j] - base) * a - off2) - sum));
-        }
-    }
-    if (p.parts > 1 && !p.backward) cluster_wait();
+    if (meet) cluster_wait();
 }
 
-template <typename T, int THREADS> cudaError_t launch_distill_threads(const DisParams &p, int rows, cudaStream_t st) {
-    return launch_pdl(distill_kernel<T, THREADS>, dim3((unsigned)rows, 1, (unsigned)p.parts), dim3(THREADS), 0, st, (unsigned)p.parts, p);
+template <typename T> cudaError_t launch_distill_type(DisParams &p, int rows, double bytes, cudaStream_t st) {
+    // Lists of up to 128 slots are compared with each other outright (64 of 4096 classes, 16384 rows: 66 us, 98 with the table; 1000 of
+    // 1000, 64 rows: 35 us, 6 with it).
+    p.table = 0;
+    if (p.dz && p.k > 128)
+        for (p.table = 2; p.table < 2 * p.k; p.table *= 2) {}
+    const unsigned list = (unsigned)(p.k * 8 + p.table * 4);
+    // Short rows, and many of them: a warp each.
+    if (bytes <= 8192 && p.k <= 128 && rows >= 8 * sm_count()) {
+        constexpr int TEAMS = 256 / 32;
+        p.parts = 1;
+        return launch_pdl(distill_kernel<T, 32, 256>, dim3((unsigned)((rows + TEAMS - 1) / TEAMS)), dim3(256), TEAMS * list, st, 1, p, rows);
+    }
+    // Blocks of 256 threads keep four rows of an SM at work, which serves the loss alone; with a gradient the rows between their two
+    // passes have to stay in L2 together with what is written: blocks of 512, two rows an SM (2048 x 65536 bf16: 123 and 109 us; the loss
+    // alone 58 and 62 us).
+    const dim3 grid((unsigned)rows, 1, (unsigned)p.parts);
+    if (p.dz && bytes / p.parts > 16384) return launch_pdl(distill_kernel<T, 512, 512>, grid, dim3(512), list, st, (unsigned)p.parts, p, rows);
+    return launch_pdl(distill_kernel<T, 256, 256>, grid, dim3(256), list, st, (unsigned)p.parts, p, rows);
 }
 
 }  // namespace
@@ -517,9 +606,7 @@ cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
     p.inv_t = 1.f / a.temperature; p.temperature = a.temperature; p.grad_scale = a.grad_scale;
     const double bytes = (double)a.classes * (a.bf16 ? 2 : 4);
     p.parts = parts_for(a.rows, bytes, 16384);
-    if (bytes <= 16384)
-        return a.bf16 ? launch_distill_threads<__nv_bfloat16, 256>(p, a.rows, st) : launch_distill_threads<float, 256>(p, a.rows, st);
-    return a.bf16 ? launch_distill_threads<__nv_bfloat16, 512>(p, a.rows, st) : launch_distill_threads<float, 512>(p, a.rows, st);
+    return a.bf16 ? launch_distill_type<__nv_bfloat16>(p, a.rows, bytes, st) : launch_distill_type<float>(p, a.rows, bytes, st);
 }
 
 }  // namespace sgs
