@@ -108,7 +108,7 @@ int parts_for(long long rows, double row_bytes, double least) {
 // that no two words are equal, larger values come first and of equal values (-0 and 0 are) the lower index.  NaN is the largest.
 //
 // A row (or part) in two passes: the k-th largest of the threads' own maxima bounds the k-th largest logit from below, and few more
-// than k logits reach it; these are collected and ranked by counting.  Rows where too many reach it (many equal values) find the
+// than k logits reach it; these are collected, from the parts of the threads whose maximum does, and ranked by counting.  Rows where too many reach it (many equal values) find the
 // k-th largest word eight bits at a time.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float v) {
@@ -146,11 +146,12 @@ struct TopParams {
     long long ldz, ldt;
 };
 
-template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(const TopParams p) {
+template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) top_logits_kernel(const TopParams p) {
     constexpr int N = Vec<T>::N, U = 4;
     __shared__ uint64_t cand[TOP_CAP];
     __shared__ uint64_t joined[8 * TOP_LOGITS_MAX];  // block 0: the parts' words
-    __shared__ int n_cand, want_s;
+    __shared__ int n_cand, n_hot, want_s, hot[THREADS];
+    __shared__ uint2 range[THREADS / 32];
     __shared__ uint64_t prefix_s;
     __shared__ int hist[256];
     const int t = threadIdx.x, part = (int)blockIdx.z, k = p.k;
@@ -161,15 +162,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 15
     const uint4 *vec = reinterpret_cast<const uint4 *>(row + s.head);
     // Calls f(vector, its first element) for this thread's vectors, f1(value, element) for its share of the edges.
     auto walk = [&](auto f, auto f1) {
-        for (int i = s.first + t; i < s.last; i += U * THREADS) {
-            uint4 q[U];
-#pragma unroll
-            for (int u = 0; u < U; u++)
-                if (i + u * THREADS < s.last) q[u] = ld_act(vec + i + u * THREADS);
-#pragma unroll
-            for (int u = 0; u < U; u++)
-                if (i + u * THREADS < s.last) f(q[u], (uint32_t)(s.head + (i + u * THREADS) * N));
-        }
+        stream<THREADS, U>(vec, s.first, s.last, t, [&](const uint4 &q, int i) { f(q, (uint32_t)(s.head + i * N)); });
         if (t < s.edges) { const long long e = s.edge(t); f1(to_float(ld_act(row + e)), (uint32_t)e); }
     };
     // Short parts, where vectors would leave threads without any logit: element by element.
@@ -188,14 +181,29 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 15
         walk([&](const uint4 &q, uint32_t) { m = max_nan(m, vec_max(q, (const T *)nullptr)); }, [&](float v, uint32_t) { m = max_nan(m, v); });
         most = key_of(m);
     }
+    // A bound that a few more than k of the maxima reach will do: halve the range of the maxima until one is found.
     uint32_t least = 0;
-    for (int b = 31; b >= (sizeof(T) == 2 ? 16 : 0); b--) {  // (the lower half of a bf16's key tells nothing: zeros, or ones below zero)
-        const uint32_t trial = least | (1u << b);
-        const int count = __syncthreads_count(most >= trial);
-        if (count >= k) least = trial;
-        if (count == k) break;
+    {
+        const uint32_t lo1 = __reduce_min_sync(0xffffffffu, most), hi1 = __reduce_max_sync(0xffffffffu, most);
+        if ((t & 31) == 0) range[t >> 5] = make_uint2(lo1, hi1);
+        __syncthreads();
+        uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+        for (int i = 0; i < THREADS / 32; i++) { lo = min(lo, range[i].x); hi = max(hi, range[i].y); }
+        const int enough = k + k / 4 + 8;
+        if (THREADS >= k && __syncthreads_count(most > 0) >= k) {
+            least = lo;  // (all reach it)
+            while (lo < hi) {
+                const uint32_t mid = lo + (hi - lo) / 2 + 1;
+                const int count = __syncthreads_count(most >= mid);
+                if (count >= k) {
+                    lo = least = mid;
+                    if (count <= enough) break;
+                } else hi = mid - 1;
+            }
+        }
     }
-    if (t == 0) n_cand = 0;
+    if (t == 0) n_cand = n_hot = 0;
     __syncthreads();
     auto take = [&](float v, uint32_t i) {
         const uint32_t key = key_of(v);
@@ -205,14 +213,32 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 15
         }
     };
     if (brief) each(take);
-    else
-        walk([&](const uint4 &q, uint32_t i) {
-            if (key_of(vec_max(q, (const T *)nullptr)) < least) return;
-            float v[N];
-            unpack(q, v);
+    else {
+        // Only the vectors of threads whose own maximum reaches the bound are read again, a warp a thread's.
+        if (most >= least) hot[atomicAdd(&n_hot, 1)] = t;  // (any order, as above)
+        __syncthreads();
+        constexpr int WARPS = THREADS / 32;
+        const int vectors = n_hot;
+        for (int h = t >> 5; h < vectors; h += U * WARPS)
+            for (int j = s.first + (t & 31) * THREADS; j < s.last; j += 32 * THREADS) {
+                uint4 q[U];
+                int at[U];
 #pragma unroll
-            for (int j = 0; j < N; j++) take(v[j], i + j);
-        }, take);
+                for (int u = 0; u < U; u++) {
+                    at[u] = h + u * WARPS < vectors ? j + hot[h + u * WARPS] : s.last;
+                    if (at[u] < s.last) q[u] = ld_act(vec + at[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    if (at[u] >= s.last || key_of(vec_max(q[u], (const T *)nullptr)) < least) continue;
+                    float v[N];
+                    unpack(q[u], v);
+#pragma unroll
+                    for (int i = 0; i < N; i++) take(v[i], (uint32_t)(s.head + (long long)at[u] * N + i));
+                }
+            }
+        if (t < s.edges) { const long long e = s.edge(t); take(to_float(ld_act(row + e)), (uint32_t)e); }
+    }
     __syncthreads();
     int n = n_cand;
     if (n > TOP_CAP) {
@@ -220,7 +246,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 15
         uint64_t prefix = 0;
         int want = k;
         for (int shift = 56; shift >= 0; shift -= 8) {
-            if (t < 256) hist[t] = 0;
+            for (int i = t; i < 256; i += THREADS) hist[i] = 0;
             __syncthreads();
             // (runs of one digit, which is what brings rows here, are added up by the thread that meets them)
             int held = -1, count = 0;
@@ -588,15 +614,22 @@ template <typename T> cudaError_t launch_distill_type(DisParams &p, int rows, do
     return launch_pdl(distill_kernel<T, 256, 256>, grid, dim3(256), list, st, (unsigned)p.parts, p, rows);
 }
 
+template <typename T> cudaError_t launch_top_type(const TopParams &p, int rows, double bytes, cudaStream_t st) {
+    const dim3 grid((unsigned)rows, 1, (unsigned)p.parts);
+    if (bytes <= 16384 && p.k <= 64 && rows >= 2 * sm_count()) return launch_pdl(top_logits_kernel<T, 128>, grid, dim3(128), 0, st, (unsigned)p.parts, p);
+    return launch_pdl(top_logits_kernel<T, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p);
+}
+
 }  // namespace
 
 cudaError_t launch_top_logits(const TopArgs &a, cudaStream_t st) {
     TopParams p;
     p.z = a.z; p.values = a.values; p.index = a.index; p.V = a.classes; p.k = a.top; p.ldz = a.ldz; p.ldt = a.ldt;
-    p.parts = parts_for(a.rows, (double)a.classes * (a.bf16 ? 2 : 4), 16384);
-    const dim3 grid((unsigned)a.rows, 1, (unsigned)p.parts);
-    if (a.bf16) return launch_pdl(top_logits_kernel<__nv_bfloat16, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p);
-    return launch_pdl(top_logits_kernel<float, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p);
+    const double bytes = (double)a.classes * (a.bf16 ? 2 : 4);
+    // (a cluster's two meetings cost as much as 64 KB of a row: 64 x 32768 bf16 takes 10.6 us with a block a row, 12.9 with two)
+    p.parts = parts_for(a.rows, bytes, 65536);
+    // Many short rows: blocks of 128 threads, eight an SM (8192 x 1000 fp32: 94 us with 512 threads, 48 with 128; 64 x 1000: 4.4 and 5.4 us).
+    return a.bf16 ? launch_top_type<__nv_bfloat16>(p, a.rows, bytes, st) : launch_top_type<float>(p, a.rows, bytes, st);
 }
 
 cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
