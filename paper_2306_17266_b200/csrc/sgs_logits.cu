@@ -62,23 +62,39 @@ template <typename T> __device__ __forceinline__ Split split_row(const T *row, i
     return s;
 }
 
-// Calls f(vector, its number) for this thread's vectors first + t, first + t + THREADS ...: the next U are on their way while U are taken.
-template <int THREADS, int U, typename F> __device__ __forceinline__ void stream(const uint4 *vec, int first, int last, int t, F f) {
-    uint4 q[U], next[U];
-    int i = first + t;
+// Calls f(vector, its number) for this thread's vectors first + t, first + t + TEAM ...  Copies into a ring of the thread's own places in
+// shared memory run STREAM_AHEAD vectors ahead: enough bytes under way for HBM's latency (two blocks of 512 threads: 144 KB an SM), which
+// registers do not hold, and nothing to wait for but the thread's own copies.
+constexpr int STREAM_STAGES = 5, STREAM_PAIR = 2, STREAM_RING = STREAM_STAGES * STREAM_PAIR;  // stages of two vectors
+__device__ __forceinline__ void copy16(uint32_t dst, const uint4 *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+template <int TEAM, int BLOCK, typename F> __device__ __forceinline__ void stream(uint4 *ring_, const uint4 *vec, int first, int last, int t, F f) {
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ring_ + threadIdx.x);
+    constexpr uint32_t STAGE = STREAM_PAIR * BLOCK * 16;
+    int ahead = first + t;  // next vector to ask for
+    auto ask = [&](uint32_t at) {
 #pragma unroll
-    for (int u = 0; u < U; u++)
-        if (i + u * THREADS < last) q[u] = ld_act(vec + i + u * THREADS);
-    for (; i < last; i += U * THREADS) {
+        for (int u = 0; u < STREAM_PAIR; u++)
+            if (ahead + u * TEAM < last) copy16(at + u * BLOCK * 16, vec + ahead + u * TEAM);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        ahead += STREAM_PAIR * TEAM;
+    };
 #pragma unroll
-        for (int u = 0; u < U; u++)
-            if (i + (U + u) * THREADS < last) next[u] = ld_act(vec + i + (U + u) * THREADS);
+    for (int d = 0; d < STREAM_STAGES - 1; d++) ask(ring + d * STAGE);
+    uint32_t at = ring, free_ = ring + (STREAM_STAGES - 1) * STAGE;
+    for (int i = first + t; i < last; i += STREAM_PAIR * TEAM) {
+        ask(free_);  // (its vectors were used in the last step)
+        asm volatile("cp.async.wait_group %0;" ::"n"(STREAM_STAGES - 1) : "memory");
+        uint4 q[STREAM_PAIR];
 #pragma unroll
-        for (int u = 0; u < U; u++)
-            if (i + u * THREADS < last) f(q[u], i + u * THREADS);
+        for (int u = 0; u < STREAM_PAIR; u++)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q[u].x), "=r"(q[u].y), "=r"(q[u].z), "=r"(q[u].w) : "r"(at + u * BLOCK * 16) : "memory");
 #pragma unroll
-        for (int u = 0; u < U; u++) q[u] = next[u];
+        for (int u = 0; u < STREAM_PAIR; u++)
+            if (i + u * TEAM < last) f(q[u], i + u * TEAM);
+        free_ = at;
+        at = at == ring + (STREAM_STAGES - 1) * STAGE ? ring : at + STAGE;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 // ---- clusters along z ------------------------------------------------------------------------------------------------------
@@ -148,8 +164,9 @@ struct TopParams {
 
 template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) top_logits_kernel(const TopParams p) {
     constexpr int N = Vec<T>::N, U = 4;
+    extern __shared__ uint4 ring[];
+    uint64_t *joined = reinterpret_cast<uint64_t *>(ring);  // block 0, when the row has been read: the parts' words
     __shared__ uint64_t cand[TOP_CAP];
-    __shared__ uint64_t joined[8 * TOP_LOGITS_MAX];  // block 0: the parts' words
     __shared__ int n_cand, n_hot, want_s, hot[THREADS];
     __shared__ uint2 range[THREADS / 32];
     __shared__ uint64_t prefix_s;
@@ -162,7 +179,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
     const uint4 *vec = reinterpret_cast<const uint4 *>(row + s.head);
     // Calls f(vector, its first element) for this thread's vectors, f1(value, element) for its share of the edges.
     auto walk = [&](auto f, auto f1) {
-        stream<THREADS, U>(vec, s.first, s.last, t, [&](const uint4 &q, int i) { f(q, (uint32_t)(s.head + i * N)); });
+        stream<THREADS, THREADS>(ring, vec, s.first, s.last, t, [&](const uint4 &q, int i) { f(q, (uint32_t)(s.head + i * N)); });
         if (t < s.edges) { const long long e = s.edge(t); f1(to_float(ld_act(row + e)), (uint32_t)e); }
     };
     // Short parts, where vectors would leave threads without any logit: element by element.
@@ -174,12 +191,20 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         for (long long i = (edges_apart ? s.head + (long long)s.first * N : 0) + t; i < last; i += THREADS) f1(to_float(ld_act(row + i)), (uint32_t)i);
         if (edges_apart && t < s.edges) { const long long e = s.edge(t); f1(to_float(ld_act(row + e)), (uint32_t)e); }
     };
-    uint32_t most = 0;  // (below every key)
+    uint32_t most = 0;  // largest key (0: below every key)
+    int top_vec = -1;   // the vector that has it
+    float second = NEG_INF;  // largest of the thread's other vectors
     if (brief) each([&](float v, uint32_t) { most = max(most, key_of(v)); });
     else {
         float m = NEG_INF;
-        walk([&](const uint4 &q, uint32_t) { m = max_nan(m, vec_max(q, (const T *)nullptr)); }, [&](float v, uint32_t) { m = max_nan(m, v); });
-        most = key_of(m);
+        stream<THREADS, THREADS>(ring, vec, s.first, s.last, t, [&](const uint4 &q, int i) {
+            const float v = vec_max(q, (const T *)nullptr);
+            const bool up = top_vec < 0 || !(v <= m);  // (the first; larger, or NaN)
+            second = max_nan(second, up ? m : v);
+            m = up ? v : m;
+            top_vec = up ? i : top_vec;
+        });
+        most = max(key_of(m), key_of(second));  // (a NaN may be behind the second)
     }
     // A bound that a few more than k of the maxima reach will do: halve the range of the maxima until one is found.
     uint32_t least = 0;
@@ -214,28 +239,24 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
     };
     if (brief) each(take);
     else {
-        // Only the vectors of threads whose own maximum reaches the bound are read again, a warp a thread's.
-        if (most >= least) hot[atomicAdd(&n_hot, 1)] = t;  // (any order, as above)
+        // Of the threads whose maximum reaches the bound most have one vector that does: it is read again; where another one does too, all
+        // of the thread's are, a warp a thread's.
+        auto look = [&](const uint4 &q, int i) {
+            float v[N];
+            unpack(q, v);
+#pragma unroll
+            for (int j = 0; j < N; j++) take(v[j], (uint32_t)(s.head + (long long)i * N + j));
+        };
+        if (most >= least) {
+            if (key_of(second) >= least) hot[atomicAdd(&n_hot, 1)] = t;  // (any order, as above)
+            else look(ld_act(vec + top_vec), top_vec);
+        }
         __syncthreads();
-        constexpr int WARPS = THREADS / 32;
-        const int vectors = n_hot;
-        for (int h = t >> 5; h < vectors; h += U * WARPS)
-            for (int j = s.first + (t & 31) * THREADS; j < s.last; j += 32 * THREADS) {
-                uint4 q[U];
-                int at[U];
-#pragma unroll
-                for (int u = 0; u < U; u++) {
-                    at[u] = h + u * WARPS < vectors ? j + hot[h + u * WARPS] : s.last;
-                    if (at[u] < s.last) q[u] = ld_act(vec + at[u]);
-                }
-#pragma unroll
-                for (int u = 0; u < U; u++) {
-                    if (at[u] >= s.last || key_of(vec_max(q[u], (const T *)nullptr)) < least) continue;
-                    float v[N];
-                    unpack(q[u], v);
-#pragma unroll
-                    for (int i = 0; i < N; i++) take(v[i], (uint32_t)(s.head + (long long)at[u] * N + i));
-                }
+        const int rescans = n_hot;
+        for (int h = t >> 5; h < rescans; h += THREADS / 32)
+            for (int i = s.first + hot[h] + (t & 31) * THREADS; i < s.last; i += 32 * THREADS) {
+                const uint4 q = ld_act(vec + i);
+                if (key_of(vec_max(q, (const T *)nullptr)) >= least) look(q, i);
             }
         if (t < s.edges) { const long long e = s.edge(t); take(to_float(ld_act(row + e)), (uint32_t)e); }
     }
@@ -407,10 +428,11 @@ struct DisParams {
 // asked for before the row is streamed and looked at behind it, the loss is summed behind the gradient, and the sums over slots that name
 // the same class are formed by the threads that own the slots while the others write.
 template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) distill_kernel(const DisParams p, const int rows) {
-    constexpr int N = Vec<T>::N, U = 4, TEAMS = BLOCK / TEAM, SLOTS = TEAM == 32 ? 4 : DISTILL_TOP_MAX / TEAM;
+    constexpr int N = Vec<T>::N, TEAMS = BLOCK / TEAM, SLOTS = TEAM == 32 ? 4 : DISTILL_TOP_MAX / TEAM;
     // a row's slots: (class, probability), class -1: not in use; then, for long lists, a table of the classes named, which tells whether one is
     // named twice
-    extern __shared__ float2 lists[];
+    extern __shared__ uint4 ring[];
+    float2 *lists = reinterpret_cast<float2 *>(ring + BLOCK * STREAM_RING);
     __shared__ int twice[TEAMS];
     __shared__ float4 joined[BLOCK / 32];
     __shared__ float sums[BLOCK / 32];
@@ -459,7 +481,7 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
             }
             return m == NEG_INF ? 0.f : -m;
         };
-        stream<TEAM, U>(vec, s.first, s.last, t, [&](const uint4 &q, int) {
+        stream<TEAM, BLOCK>(ring, vec, s.first, s.last, t, [&](const uint4 &q, int) {
             float v[N];
             unpack(q, v);
             const float b = raise(vec_most(q, (const T *)nullptr));
@@ -554,7 +576,7 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
             }
         };
         if (c != 0.f)
-            stream<TEAM, U>(vec, s.first, s.last, t, [&](const uint4 &q, int i) {
+            stream<TEAM, BLOCK>(ring, vec, s.first, s.last, t, [&](const uint4 &q, int i) {
                 float v[N];
                 unpack(q, v);
 #pragma unroll
@@ -593,6 +615,13 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
     if (meet) cluster_wait();
 }
 
+template <typename T, int TEAM, int BLOCK> cudaError_t launch_distill_blocks(const DisParams &p, dim3 grid, unsigned list, int rows, cudaStream_t st) {
+    constexpr unsigned RING = BLOCK * STREAM_RING * 16, LISTS = (TEAM == 32 ? 8 * 128 : DISTILL_TOP_MAX) * 16;  // (a slot and its places in the table)
+    static DeviceBits done;
+    cudaError_t e = smem_limit_once(distill_kernel<T, TEAM, BLOCK>, RING + LISTS, done);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(distill_kernel<T, TEAM, BLOCK>, grid, dim3(BLOCK), RING + list, st, (unsigned)p.parts, p, rows);
+}
 template <typename T> cudaError_t launch_distill_type(DisParams &p, int rows, double bytes, cudaStream_t st) {
     // Lists of up to 128 slots are compared with each other outright (64 of 4096 classes, 16384 rows: 66 us, 98 with the table; 1000 of
     // 1000, 64 rows: 35 us, 6 with it).
@@ -604,20 +633,25 @@ template <typename T> cudaError_t launch_distill_type(DisParams &p, int rows, do
     if (bytes <= 8192 && p.k <= 128 && rows >= 8 * sm_count()) {
         constexpr int TEAMS = 256 / 32;
         p.parts = 1;
-        return launch_pdl(distill_kernel<T, 32, 256>, dim3((unsigned)((rows + TEAMS - 1) / TEAMS)), dim3(256), TEAMS * list, st, 1, p, rows);
+        return launch_distill_blocks<T, 32, 256>(p, dim3((unsigned)((rows + TEAMS - 1) / TEAMS)), TEAMS * list, rows, st);
     }
     // Blocks of 256 threads keep four rows of an SM at work, which serves the loss alone; with a gradient the rows between their two
     // passes have to stay in L2 together with what is written: blocks of 512, two rows an SM (2048 x 65536 bf16: 123 and 109 us; the loss
     // alone 58 and 62 us).
     const dim3 grid((unsigned)rows, 1, (unsigned)p.parts);
-    if (p.dz && bytes / p.parts > 16384) return launch_pdl(distill_kernel<T, 512, 512>, grid, dim3(512), list, st, (unsigned)p.parts, p, rows);
-    return launch_pdl(distill_kernel<T, 256, 256>, grid, dim3(256), list, st, (unsigned)p.parts, p, rows);
+    if (p.dz && bytes / p.parts > 16384) return launch_distill_blocks<T, 512, 512>(p, grid, list, rows, st);
+    return launch_distill_blocks<T, 256, 256>(p, grid, list, rows, st);
 }
 
 template <typename T> cudaError_t launch_top_type(const TopParams &p, int rows, double bytes, cudaStream_t st) {
     const dim3 grid((unsigned)rows, 1, (unsigned)p.parts);
-    if (bytes <= 16384 && p.k <= 64 && rows >= 2 * sm_count()) return launch_pdl(top_logits_kernel<T, 128>, grid, dim3(128), 0, st, (unsigned)p.parts, p);
-    return launch_pdl(top_logits_kernel<T, 512>, grid, dim3(512), 0, st, (unsigned)p.parts, p);
+    if (bytes <= 16384 && p.k <= 64 && rows >= 2 * sm_count())  // (rows that are read element by element need no ring)
+        return launch_pdl(top_logits_kernel<T, 128>, grid, dim3(128), p.V <= 2 * Vec<T>::N * 128 ? 0 : 128 * STREAM_RING * 16, st, 1, p);
+    static_assert(512 * STREAM_RING * 16 >= 8 * TOP_LOGITS_MAX * 8, "the parts' words");
+    static DeviceBits done;
+    cudaError_t e = smem_limit_once(top_logits_kernel<T, 512>, 512 * STREAM_RING * 16, done);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(top_logits_kernel<T, 512>, grid, dim3(512), 512 * STREAM_RING * 16, st, (unsigned)p.parts, p);
 }
 
 }  // namespace
