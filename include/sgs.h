@@ -535,6 +535,17 @@ sgs_status_t sgs_distill_backward(const sgs_distill_desc_t *desc, const void *d_
  * writes; outputs must not overlap inputs (but for dz = z).  Pointers are of the current device (SGS_EINVAL for another device's
  * and for host memory that the device cannot read). */
 
+/*
+ * sgs_subnet_divergence - how far the answers of n_subnets SubNets are from a teacher SubNet's (normally the largest) on a batch of
+ * images: divergence[i] (host doubles) = mean over the images of sgs_distill's loss of SubNet i's logits against the teacher's `top`
+ * largest, at `temperature`.  It needs no labels: with its sign turned it is an accuracy proxy for sgs_sched_create (Section 3.2: the
+ * scheduler ranks SubNets by accuracy).  d_input [batch][res][res][3] in the compute dtype.  The cached SubGraph and its policy are left
+ * as they are.  Allocates while it runs, and synchronises `cuda_stream`, so it refuses a stream under capture.
+ * Errors: SGS_EINVAL, SGS_ECONFIG, SGS_ENOMEM, SGS_ECUDA, SGS_ETIMEOUT.
+ */
+sgs_status_t sgs_subnet_divergence(sgs_supernet_t *net, const sgs_subnet_cfg_t *teacher, const sgs_subnet_cfg_t *subnets, int n_subnets,
+                                   const void *d_input, int batch, int res, int top, float temperature, double *divergence, void *cuda_stream);
+
 /* Nonzero once a kernel of this process has reported that one of its bounded waits ran out (the paper has no
  * counterpart: every device-side wait of the kernels carries a time limit, after which the kernel records the fact
  * in a status word of its device, lets its copies land, frees its tensor memory and returns; calls that follow

@@ -28,7 +28,7 @@ EXPORTS = [
     "sgs_profile_read", "sgs_conv2d_sliced_static", "sgs_cache_set_candidates", "sgs_cache_set_policy",
     "sgs_sched_create", "sgs_sched_free", "sgs_sched_dims", "sgs_sched_set_table", "sgs_sched_get_table", "sgs_sched_measure",
     "sgs_sched_step", "sgs_sched_subnet", "sgs_profile_trace", "sgs_layer_name", "sgs_aux_op", "sgs_device_status_clear", "sgs_debug_expire_wait", "sgs_debug_expire_team_wait", "sgs_debug_pointwise_tiles", "sgs_debug_layer_map", "sgs_measure_fma_peak", "sgs_conv2d_sliced_i8",
-    "sgs_quantize_f8", "sgs_linear_f8", "sgs_top_logits", "sgs_distill", "sgs_distill_backward",
+    "sgs_quantize_f8", "sgs_linear_f8", "sgs_top_logits", "sgs_distill", "sgs_distill_backward", "sgs_subnet_divergence",
 ]
 
 
@@ -236,6 +236,7 @@ def lib():
         L.sgs_top_logits.argtypes = [vp] * 5
         L.sgs_distill.argtypes = [vp] * 9
         L.sgs_distill_backward.argtypes = [vp] * 8
+        L.sgs_subnet_divergence.argtypes = [vp, vp, vp, ci, vp, ci, ci, ci, ctypes.c_float, vp, vp]
         _lib = L
     return _lib
 
@@ -381,6 +382,16 @@ class SuperNet:
 
     def subnet_run(self, cfg: SubnetCfg, d_input: int, batch: int, res: int, d_logits: int, stream: int = 0):
         self._check(lib().sgs_subnet_run(self._h, ctypes.byref(cfg), d_input, batch, res, d_logits, stream))
+
+    def subnet_divergence(self, teacher: SubnetCfg, subnets: Sequence[SubnetCfg], d_input: int, batch: int, res: int, top: int = 32,
+                          temperature: float = 4.0, stream: int = 0):
+        """Mean distillation loss of every SubNet against the teacher's top logits; minus this is an accuracy proxy for Scheduler."""
+        import numpy as np
+        arr = subnets if isinstance(subnets, ctypes.Array) else cfg_array(subnets)
+        out = np.zeros(len(arr), dtype=np.float64)
+        self._check(lib().sgs_subnet_divergence(self._h, ctypes.byref(teacher), ctypes.addressof(arr), len(arr), d_input, batch, res, top, temperature,
+                                                out.ctypes.data, stream))
+        return out
 
     def stream_run(self, cfgs: Sequence[SubnetCfg], d_inputs, batch: int, res: int, d_logits,
                    opts: Optional[StreamOpts] = None, stream: int = 0, host: bool = False) -> StreamStats:

@@ -3056,4 +3056,57 @@ sgs_status_t sgs_distill_backward(const sgs_distill_desc_t *desc, const void *d_
     return distill(desc, d_z, d_teacher, d_index, d_row_scale, nullptr, const_cast<float *>(d_stat), d_dz, 1, cuda_stream);
 } SGS_NO_THROW
 
+// How far SubNets' answers are from a teacher SubNet's (see sgs.h): the queries as sgs_sched_measure runs them, then the operators above.
+sgs_status_t sgs_subnet_divergence(sgs_supernet_t *net, const sgs_subnet_cfg_t *teacher, const sgs_subnet_cfg_t *subnets, int n_subnets, const void *d_input,
+                                   int batch, int res, int top, float temperature, double *divergence, void *cuda_stream) try {
+    if (!net) return SGS_EINVAL;
+    if (!teacher || !subnets || n_subnets < 1 || !d_input || !divergence || batch <= 0 || res < 8 || res > 1024) return fail(net, SGS_EINVAL, "bad argument");
+    const int classes = net->def.classes;
+    if (top < 1 || top > classes || top > TOP_LOGITS_MAX || !(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
+        return fail(net, SGS_EINVAL, "top or temperature out of range");
+    if (!cfg_valid(net, teacher)) return fail(net, SGS_ECONFIG, "teacher: config outside the elastic sets");
+    for (int i = 0; i < n_subnets; i++)
+        if (!cfg_valid(net, &subnets[i])) return fail(net, SGS_ECONFIG, "SubNet " + std::to_string(i) + ": config outside the elastic sets");
+    DeviceGuard guard(net->device);
+    if (!guard.ok) return fail(net, SGS_ECUDA, "cudaSetDevice failed");
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (being_captured(st)) return fail(net, SGS_EINVAL, "the stream is being captured, and this call synchronises it");
+    if (net->stop_after_layer >= 0) return fail(net, SGS_EINVAL, "option stop_after_layer leaves no logits");
+    std::vector<float> losses((size_t)n_subnets * batch);
+    const size_t logits_b = (size_t)batch * classes * 4, list_b = (size_t)batch * top * 4, loss_b = losses.size() * 4;
+    struct Buffer {  // (freed on every way out)
+        sgs_supernet *net;
+        void *p = nullptr;
+        size_t bytes;
+        ~Buffer() { dev_free(net, p, bytes); }
+    } buf{net, nullptr, logits_b + 2 * list_b + loss_b};
+    sgs_status_t rc = dev_alloc(net, &buf.p, buf.bytes);
+    if (rc != SGS_OK) return rc;
+    char *at = static_cast<char *>(buf.p);
+    float *logits = reinterpret_cast<float *>(at), *values = reinterpret_cast<float *>(at + logits_b), *loss = reinterpret_cast<float *>(at + logits_b + 2 * list_b);
+    int *index = reinterpret_cast<int *>(at + logits_b + list_b);
+    TopArgs ta;
+    ta.z = logits; ta.values = values; ta.index = index; ta.rows = batch; ta.classes = classes; ta.top = top; ta.ldz = classes; ta.ldt = top;
+    DistillArgs da;
+    da.z = logits; da.teacher = values; da.index = index; da.rows = batch; da.classes = classes; da.top = top;
+    da.ldz = da.lddz = classes; da.ldt = top; da.temperature = temperature;
+    rc = run_query(net, teacher, d_input, batch, res, logits, st, false, 0, nullptr);
+    if (rc == SGS_OK && launch_top_logits(ta, st) != cudaSuccess) rc = fail(net, SGS_ECUDA, "top logits failed");
+    for (int i = 0; i < n_subnets && rc == SGS_OK; i++) {
+        rc = run_query(net, &subnets[i], d_input, batch, res, logits, st, false, 0, nullptr);
+        da.loss = loss + (size_t)i * batch;
+        if (rc == SGS_OK && launch_distill(da, st) != cudaSuccess) rc = fail(net, SGS_ECUDA, "distillation loss failed");
+    }
+    if (rc == SGS_OK && cudaMemcpyAsync(losses.data(), loss, loss_b, cudaMemcpyDeviceToHost, st) != cudaSuccess) rc = fail(net, SGS_ECUDA, "copy of the losses failed");
+    if (cudaStreamSynchronize(st) != cudaSuccess && rc == SGS_OK) rc = fail(net, SGS_ECUDA, "stream synchronise failed");
+    if (rc == SGS_OK && tc_conv_status()) return fail(net, SGS_ETIMEOUT, "a bounded wait ran out in a tensor-core kernel");
+    if (rc != SGS_OK) return rc;
+    for (int i = 0; i < n_subnets; i++) {
+        double sum = 0;
+        for (int b = 0; b < batch; b++) sum += losses[(size_t)i * batch + b];
+        divergence[i] = sum / batch;
+    }
+    return SGS_OK;
+} SGS_NO_THROW
+
 }  // extern "C"

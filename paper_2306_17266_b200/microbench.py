@@ -4,8 +4,10 @@
     python -m paper_2306_17266_b200.microbench conv --shape 1,7,7,720,720,720,720,3,3,1 --once 3
     python -m paper_2306_17266_b200.microbench conv-i8 --preset resnet_b16
     python -m paper_2306_17266_b200.microbench dw --preset large
+    python -m paper_2306_17266_b200.microbench linear-f8 --shape 12544,408,512
 
-conv shapes: N,H,W,Cmax,C,Kmax,K,R,k,stride; dw shapes: N,H,W,K,k,stride (stored kernel 7x7).
+conv shapes: N,H,W,Cmax,C,Kmax,K,R,k,stride; dw shapes: N,H,W,K,k,stride (stored kernel 7x7); linear-f8 shapes: M,K,C (rows, filters,
+channels; the operands are quantised by sgs_quantize_f8, which is timed too).
 Times are CUDA events around a captured graph of back-to-back launches (conv) or a plain launch loop
 (dw, working sets larger than L2).  `--once n` just runs n launches (for profilers).
 """
@@ -29,6 +31,10 @@ CONV_PRESETS = {
 DW_PRESETS = {
     "large": [(64, 56, 56, 480, k, s) for k in (3, 5, 7) for s in (1, 2)] + [(128, 28, 28, 672, k, 1) for k in (3, 5, 7)],
     "b1": [(1, 112, 112, 96, 3, 2), (1, 28, 28, 240, 5, 1), (1, 14, 14, 672, 7, 1)],
+}
+LINEAR_F8_PRESETS = {
+    # pointwise layers of the ResNet-50-shaped SuperNet on 16 images, its classifier, one row of a wide layer
+    "resnet_b16": [(50176, 64, 64), (50176, 256, 88), (12544, 512, 176), (3136, 1024, 360), (784, 2048, 720), (16, 1000, 2048), (1, 8192, 4096)],
 }
 
 
@@ -116,6 +122,43 @@ def bench_conv_i8(shape, iters=200):
     return {"shape": (N, H, W, Cmax, C, Kmax, K, R, k, stride), "us": us, "tops": ops / us / 1e6, "gbs": nbytes / us / 1e3}
 
 
+def bench_linear_f8(shape, iters=100):
+    """Quantisation of the rows, and the layer on 8-bit floating point operands (sgs_quantize_f8, sgs_linear_f8)."""
+    M, K, C = shape
+    ld, cb = (C + 15) // 16 * 16, (C + 127) // 128
+    x = torch.randn(M, C, device="cuda").to(torch.bfloat16)
+    w = torch.randn(K, C, device="cuda").to(torch.bfloat16)
+    xq, wq = torch.empty((M, ld), device="cuda", dtype=torch.uint8), torch.empty((K, ld), device="cuda", dtype=torch.uint8)
+    sx, sw = torch.empty((cb, M), device="cuda"), torch.empty((cb, (K + 127) // 128), device="cuda")
+    y = torch.empty((M, K), device="cuda", dtype=torch.bfloat16)
+    dx = sgs.QuantizeF8Desc(rows=M, cols=C, dtype=sgs.SGS_BF16, format=sgs.SGS_E4M3, block_rows=1)
+    dw = sgs.QuantizeF8Desc(rows=K, cols=C, dtype=sgs.SGS_BF16, format=sgs.SGS_E4M3, block_rows=128)
+    d = sgs.LinearF8Desc(M=M, K=K, C=C, Kmax=K, Cmax=C, w_block_rows=128, y_dtype=sgs.SGS_BF16)
+    st = torch.cuda.Stream()
+    calls = [lambda: sgs.quantize_f8(dx, x.data_ptr(), xq.data_ptr(), sx.data_ptr(), stream=st.cuda_stream),
+             lambda: sgs.linear_f8(d, xq.data_ptr(), sx.data_ptr(), wq.data_ptr(), sw.data_ptr(), 0, y.data_ptr(), st.cuda_stream)]
+    torch.cuda.synchronize()
+    sgs.quantize_f8(dw, w.data_ptr(), wq.data_ptr(), sw.data_ptr(), stream=st.cuda_stream)
+    us = []
+    for call in calls:
+        for _ in range(3):
+            call()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            for _ in range(iters):
+                call()
+        g.replay()
+        torch.cuda.synchronize()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        g.replay()
+        e1.record()
+        torch.cuda.synchronize()
+        us.append(e0.elapsed_time(e1) * 1000 / iters)
+    return {"shape": shape, "quantize_us": us[0], "us": us[1], "tflops": 2.0 * M * K * C / us[1] / 1e6, "gbs": (M * C + K * C + 2.0 * M * K) / us[1] / 1e3}
+
+
 def bench_dw(shape, iters=20, once=0):
     N, H, W, K, k, stride = shape
     p = (k - 1) // 2
@@ -178,7 +221,7 @@ def wave_trace(family, wave, queries, res, batch):
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("kind", choices=["conv", "conv-i8", "dw", "trace"])
+    ap.add_argument("kind", choices=["conv", "conv-i8", "dw", "linear-f8", "trace"])
     ap.add_argument("--family", default="resnet", choices=["resnet", "mbv3"])
     ap.add_argument("--wave", type=int, default=32)
     ap.add_argument("--queries", type=int, default=128)
@@ -195,13 +238,16 @@ def main():
     if args.shape:
         shapes = [tuple(int(v) for v in args.shape.split(","))]
     else:
-        table = DW_PRESETS if args.kind == "dw" else CONV_PRESETS
-        shapes = table[args.preset or ("large" if args.kind == "dw" else "resnet_b1")]
+        table, default = {"dw": (DW_PRESETS, "large"), "linear-f8": (LINEAR_F8_PRESETS, "resnet_b16")}.get(args.kind, (CONV_PRESETS, "resnet_b1"))
+        shapes = table[args.preset or default]
     for sh in shapes:
         if args.kind == "conv-i8":
             r = bench_conv_i8(sh)
             sh = r["shape"]
             print(f"conv-i8 N{sh[0]} {sh[1]}x{sh[2]} C{sh[4]} K{sh[6]} k{sh[8]} s{sh[9]}: {r['us']:8.2f} us  {r['tops']:8.2f} TOP/s  {r['gbs']:8.1f} GB/s", flush=True)
+        elif args.kind == "linear-f8":
+            r = bench_linear_f8(sh)
+            print(f"linear-f8 M{sh[0]} K{sh[1]} C{sh[2]}: {r['us']:8.2f} us  {r['tflops']:8.2f} TFLOP/s  {r['gbs']:8.1f} GB/s   (rows quantised in {r['quantize_us']:.2f} us)", flush=True)
         elif args.kind == "conv":
             r = bench_conv(sh, once=args.once, split_off=args.split_off)
             if r:
