@@ -152,11 +152,23 @@ struct QuantParams {
 template <typename T, bool E5M2> __device__ __forceinline__ uint2 codes8(const Eight<T> &e, float inv) {
     return make_uint2(codes4<E5M2>(e.at(0) * inv, e.at(1) * inv, e.at(2) * inv, e.at(3) * inv), codes4<E5M2>(e.at(4) * inv, e.at(5) * inv, e.at(6) * inv, e.at(7) * inv));
 }
-__device__ __forceinline__ uint32_t half_warp_max(uint32_t a) {
+// Largest of each of R rows over the 16 threads that hold them; a thread is left with one row's, row_of(l) (16 / R threads hold the same).
+// The first exchanges halve what a thread still has: R + log2(16 / R) - 1 shuffles in place of 4 R.
+template <int R> __device__ __forceinline__ uint32_t rows_max(uint32_t (&m)[R], int l) {
+    int o = 8;
 #pragma unroll
-    for (int o = 8; o; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
-    return a;
+    for (int n = R / 2; n >= 1; n /= 2, o /= 2) {
+        const bool high = l & o;
+#pragma unroll
+        for (int i = 0; i < n; i++) {
+            const uint32_t send = high ? m[i] : m[i + n], keep = high ? m[i + n] : m[i];
+            m[i] = max(keep, __shfl_xor_sync(0xffffffffu, send, o));
+        }
+    }
+    for (; o; o /= 2) m[0] = max(m[0], __shfl_xor_sync(0xffffffffu, m[0], o));
+    return m[0];
 }
+template <int R> __device__ __forceinline__ int row_of(int l) { return l / (16 / R); }
 
 // Row-wise codes alone, a scale per 128 elements: 16 threads take a block of each of four neighbouring rows; nothing is shared.
 constexpr int QROWS = 4;
@@ -174,26 +186,34 @@ template <typename T, bool E5M2> __global__ void __launch_bounds__(256) quantize
         const bool in = r0 + i < p.rows && n > 0;
         v[i].load(static_cast<const T *>(p.x) + (in ? (long long)(r0 + i) * p.ldx + c0 : 0), in ? n : 0, p.vec_x);
     }
+    uint32_t m[QROWS];
 #pragma unroll
-    for (int i = 0; i < QROWS; i++) {
-        uint32_t a = half_warp_max(v[i].most());
-        if (__any_sync(0xffffffffu, a >= INF_BITS)) {  // (rare; for both half-warps, whose shuffles are one instruction)
-            a = half_warp_max(v[i].most_finite());
+    for (int i = 0; i < QROWS; i++) m[i] = v[i].most();
+    uint32_t a = rows_max<QROWS>(m, l);
+    if (__any_sync(0xffffffffu, a >= INF_BITS)) {  // (rare; for both half-warps, whose shuffles are one instruction)
+#pragma unroll
+        for (int i = 0; i < QROWS; i++) {
+            m[i] = v[i].most_finite();
             v[i].set_nan();
         }
-        const int field = scale_field(a, TOP);
-        const uint2 q = codes8<T, E5M2>(v[i], inverse_of(field));
+        a = rows_max<QROWS>(m, l);
+    }
+    const int field = scale_field(a, TOP), mine = row_of<QROWS>(l);
+    if (l % (16 / QROWS) == 0 && r0 + mine < p.rows) p.scale[(long long)ct * p.lds + r0 + mine] = scale_of(field);
+    const float own = inverse_of(field);
+#pragma unroll
+    for (int i = 0; i < QROWS; i++) {
+        const uint2 q = codes8<T, E5M2>(v[i], __shfl_sync(0xffffffffu, own, (t & 16) + i * (16 / QROWS)));
         if (r0 + i < p.rows && n > 0) {
             uint8_t *dst = p.q + (long long)(r0 + i) * p.ldq + c0;
             if (p.vec_q && n == 8) *reinterpret_cast<uint2 *>(dst) = q;
             else store_bytes(dst, q.x, q.y, n);
-            if (l == 0) p.scale[(long long)ct * p.lds + r0 + i] = scale_of(field);
         }
     }
 }
 
 template <typename T, bool E5M2, bool SQUARE, bool ROWS, bool TRANSPOSED>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) quantize_f8_kernel(const QuantParams p) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_f8_kernel(const QuantParams p) {
     __shared__ __align__(16) uint8_t tile[TRANSPOSED ? 128 * 128 : 16];
     __shared__ uint32_t col_max[TRANSPOSED && !SQUARE ? 16 : 1][128];
     __shared__ uint32_t warp_max[8];
@@ -258,14 +278,18 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) quantize_f8_kerne
         }
     }
     if (ROWS) {
+        float own = inverse_of(square);
+        if (!SQUARE) {
+            uint32_t m[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) m[i] = odd ? v[i].most_finite() : v[i].most();
+            const int field = scale_field(rows_max<8>(m, l), TOP), mine = row_of<8>(l);
+            if (l % 2 == 0 && r0 + mine < p.rows) p.scale[(long long)ct * p.lds + r0 + mine] = scale_of(field);
+            own = inverse_of(field);
+        }
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            int field = square;
-            if (!SQUARE) {
-                field = scale_field(half_warp_max(odd ? v[i].most_finite() : v[i].most()), TOP);
-                if (l == 0 && r0 + i < p.rows) p.scale[(long long)ct * p.lds + r0 + i] = scale_of(field);
-            }
-            const uint2 q = codes8<T, E5M2>(v[i], inverse_of(field));
+            const uint2 q = codes8<T, E5M2>(v[i], SQUARE ? own : __shfl_sync(0xffffffffu, own, (t & 16) + 2 * i));
             if (r0 + i < p.rows && n > 0) {
                 uint8_t *dst = p.q + (long long)(r0 + i) * p.ldq + c0;
                 if (p.vec_q && n == 8) *reinterpret_cast<uint2 *>(dst) = q;
