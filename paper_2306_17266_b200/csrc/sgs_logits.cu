@@ -512,7 +512,7 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
         if (at[q] < 0) continue;
         teach = join(teach, make_float2(tv[q] == tv[q] ? tv[q] : NEG_INF, tv[q] == tv[q] ? 1.f : tv[q]), a);
         if (p.table)
-            for (int h = at[q] * 40503 & (p.table - 1);; h = (h + 1) & (p.table - 1)) {  // (never full: it has at least twice as many places as slots)
+            for (int h = (int)((unsigned)at[q] * 40503u) & (p.table - 1);; h = (h + 1) & (p.table - 1)) {  // (never full: it has at least twice as many places as slots)
                 const int there = atomicCAS(&table[h], -1, at[q]);
                 if (there == at[q]) twice[team] = 1;
                 if (there == -1 || there == at[q]) break;
