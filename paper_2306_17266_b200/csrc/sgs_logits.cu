@@ -63,9 +63,9 @@ template <typename T> __device__ __forceinline__ Split split_row(const T *row, i
 }
 
 // Calls f(vector, its number) for this thread's vectors first + t, first + t + TEAM ...  Copies into a ring of the thread's own places in
-// shared memory run STREAM_AHEAD vectors ahead: enough bytes under way for HBM's latency (two blocks of 512 threads: 144 KB an SM), which
+// shared memory run STREAM_AHEAD vectors ahead: enough bytes under way for HBM's latency (two blocks of 512 threads: 128 KB an SM), which
 // registers do not hold, and nothing to wait for but the thread's own copies.
-constexpr int STREAM_STAGES = 5, STREAM_PAIR = 2, STREAM_RING = STREAM_STAGES * STREAM_PAIR;  // stages of two vectors
+constexpr int STREAM_STAGES = 4, STREAM_PAIR = 2, STREAM_RING = STREAM_STAGES * STREAM_PAIR;  // stages of two vectors
 template <bool LAST_USE> __device__ __forceinline__ void copy16(uint32_t dst, const uint4 *src, uint64_t policy) {  // LAST_USE: with an L2 policy
     if (LAST_USE) asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
     else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
