@@ -5,6 +5,16 @@
 // The tensor core sums the 128 products of a block; the scales differ from block to block, so a block's sums have to leave the
 // tensor memory and be added up in registers: acc += (sx * sw) * t, in fp32.  Slices are extents of the tensor maps: the first K
 // rows and C columns of the stored weights, zeros beyond.
+//
+// Three forms, by the size of the call: pairs of blocks on tiles of 256 x 256 where those fill the GPU, single blocks on tiles of 128 x 128,
+// and for up to 64 rows, or fewer tiles than SMs, tiles of 128 rows of w whose reduction a cluster shares.
+//
+// What bounds the large form (8192^3, 585 us, 1.88 PFLOP/s at some 1.55 GHz under the power cap): the way of a block's sums through the
+// warps.  The MMAs of a block take 512 clocks; with the sums left out a block takes 745 (operand copies and MMAs share the port of shared
+// memory, and each accumulator passes from hand to hand), with them 1030: a wait, four loads of the tensor memory and 64 packed
+// multiply-adds are a chain that two warps a scheduler do not hide.  Measured instead (same call, 598 us then): sixteen warps of 64 columns
+// 602 us; tiles of 256 x 192 with twelve warps that read all their columns first 610 us; 256 x 160 with three accumulators 676 us; two teams
+// of warps on alternate blocks of 256 x 128 tiles 935 us; scalar multiply-adds 595 us.
 #include "sgs_tc.cuh"
 
 #include <algorithm>
@@ -128,7 +138,7 @@ template <int N> __device__ __forceinline__ void store_row(const F8Params &p, lo
 
 // A tile is 128 rows of x a block (lanes of the tensor memory) x BN rows of w (columns); CTAS = 2: the blocks of a cluster of two share
 // a tile of 256 rows, each holds its rows of x and half of the rows of w, and the first one issues the MMAs for both.
-// Warp 0 loads, warp 1 issues, warps 4..11 add up: a quadrant of the lanes and half of the columns each.  512 / BN accumulators: the
+// Warp 0 loads, warp 1 issues, warp 2 brings the scales, warps 4..11 add up: a quadrant of the lanes and half of the columns each.  512 / BN accumulators: the
 // tensor core sums a block into one while the warps take another, and into the next tile's while they write this one's.
 template <int CTAS, int BN, bool W_ROWS>
 __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_constant__ F8Params p) {
@@ -268,6 +278,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             bool ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag);
             tc_fence_after();
             if (ok) tmem_ld32(taddr + (uint32_t)(a * BN), v[0]);
+            // (four blocks written out where registers allow: 1024x4096x4096, 29.9 us and 24.8; the pairs' kernel spills, 584 and 607 us at 8192^3)
+#pragma unroll(CTAS == 1 ? F8_AHEAD : 1)
             for (int b = 0; ok && b < blocks; b++) {
                 const int k = b % F8_AHEAD;
                 if (k == 0) {
@@ -293,7 +305,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                     else {
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) arrive_at(drained0 + (uint32_t)(a * 8));
+                        if (lane == 0) {
+                            if (CTAS == 1) mbar_arrive(&sh.acc_empty[a]);
+                            else arrive_at(drained0 + (uint32_t)(a * 8));
+                        }
                         if (++a == NACC) { a = 0; acc_phase ^= 1; }
                         if (b + 1 < blocks) {
                             ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag);
@@ -396,7 +411,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
 
 // Few rows of x: the rows of w take the lanes (128 a block), up to N rows of x the columns, and the blocks of a cluster share the
 // reduction, whose parts meet in distributed shared memory, in the order of c.  What bounds such a call is w's bytes: 16 KB of them a
-// stage, two thread blocks an SM.  Warp 0 loads, 1 issues, 2 brings the scales, warps 4..7 add up, a quadrant of the lanes each.
+// stage, two thread blocks an SM (one row, 8192 filters, 4096 channels: 9.3 us, 3.6 TB/s; 16384 x 8192: 57 % of the DRAM rate; the rest is
+// the way in and out: launch, first copies, the cluster's two meetings).  Blocks that share an SM hold 256 columns of tensor memory at most
+// each, and kernels that fit beside them the rest: no allocation waits for another block's, which a cluster whose blocks wait for each
+// other could not afford.  Warp 0 loads, 1 issues, 2 brings the scales, warps 4..7 add up, a quadrant of the lanes each.
 constexpr int F8_SPLIT_THREADS = 256, F8_SPLIT_RING = 96 * 1024;
 struct F8Split {
     int parts, part_blocks;  // blocks of a cluster; blocks of the reduction that each of them takes (the last may have fewer)
@@ -594,6 +612,7 @@ template <int N, bool W_ROWS> cudaError_t launch_split(F8Params &p, const Linear
     const unsigned filters = (unsigned)((a.K + TILE_M - 1) / TILE_M), rows = (unsigned)((a.M + N - 1) / N);
     F8Split q;
     q.parts = 1;
+    // (one row, 8192 x 4096: 9.3 us with 4 parts, 10.0 with 2, 12.8 with 8)
     while (q.parts < 8 && (long long)filters * rows * q.parts < sm_count() && p.blocks >= 4 * q.parts) q.parts *= 2;
     q.part_blocks = (p.blocks + q.parts - 1) / q.parts;
     while ((q.parts - 1) * q.part_blocks >= p.blocks) q.parts--;  // (no block without a share; any number makes a cluster)
@@ -642,6 +661,7 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
         p.bulk_y = a.K / unit * unit;
     p.formats = ((uint32_t)(a.x_e5m2 ? 1 : 0) << 7) | ((uint32_t)(a.w_e5m2 ? 1 : 0) << 10);
     const long long tiles = (long long)((a.M + 127) / 128) * ((a.K + 127) / 128);
+    // (layers with fewer tiles than SMs: 128 x 4096 x 4096 takes 15 us split, 28 in tiles of 128 x 128 on 32 SMs)
     if (a.M <= 16) return a.w_rows ? launch_split<16, true>(p, a, g_set[4], st) : launch_split<16, false>(p, a, g_set[5], st);
     if (a.M <= 32) return a.w_rows ? launch_split<32, true>(p, a, g_set[6], st) : launch_split<32, false>(p, a, g_set[7], st);
     if (a.M <= 64 || tiles < sm_count()) return a.w_rows ? launch_split<64, true>(p, a, g_set[8], st) : launch_split<64, false>(p, a, g_set[9], st);
