@@ -2,10 +2,13 @@
 //
 // Both read rows of some thousand to some hundred thousand logits and are bound by bytes where there are many rows and by a chain of
 // latencies where there are few.  Hence for both: a row is one block's, or the blocks of a cluster take contiguous parts of it and meet
-// through distributed shared memory where the rows alone do not fill the GPU; 16-byte loads, four in flight a thread, from the first
-// aligned element of a row on (rows of an odd pitch start anywhere); a second pass over the same row instead of keeping it (three
-// blocks of an SM hold about 1 MB of rows at a time between the two passes on all SMs together, which stays in the 126 MB L2: HBM
-// sees one read).
+// through distributed shared memory where the rows alone do not fill the GPU; copies of 16 bytes into shared memory run ahead of their
+// use, from the first aligned element of a row on (rows of an odd pitch start anywhere); and a second pass reads a row again instead of
+// keeping it: two blocks an SM are between their passes with 39 MB of rows of 128 KB, which stay in the 126 MB L2 (four blocks an SM, and
+// what they write, do not: 2048 x 65536 bf16 takes 123 us then, 110 with two).
+// Measured (B200): top 64 of 512 x 131071 bf16 31.8 us (4.2 TB/s), fp32 51 us (5.2 TB/s); loss and gradient of 2048 x 65536 bf16 110 us
+// (4.9 TB/s of what has to be read and written), fp32 201 us (5.4 TB/s); the loss alone 52 us; the gradient of 1000 x 100008 bf16 71.5 us
+// (5.6 TB/s); the loss of 64 x 1000 fp32 3.1 us.
 #include "sgs_internal.h"
 #include "sgs_pdl.cuh"
 
