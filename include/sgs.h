@@ -516,7 +516,7 @@ sgs_status_t sgs_top_logits(const sgs_top_logits_desc_t *desc, const void *d_z, 
  *   d_loss fp32 [rows]     d_stat fp32 [rows][2] or NULL: the row's largest logit and log sum exp((z - largest) / T)
  *   d_dz NULL: the loss alone.  d_dz may be d_z with the same pitch (the gradient replaces the logits).
  * sgs_distill_backward - dz alone, from the statistics that sgs_distill left; T, lists and logits as then.
- * 1 <= top <= SGS_DISTILL_TOP_MAX, 0 < T < infinity, grad_scale finite.
+ * 1 <= top <= SGS_DISTILL_TOP_MAX, 0 < T < infinity and 1.5 / T finite, grad_scale finite.
  */
 #define SGS_DISTILL_TOP_MAX 1024
 typedef struct {

@@ -3028,7 +3028,7 @@ static sgs_status_t distill(const sgs_distill_desc_t *d, const void *d_z, const 
                             float *d_loss, float *d_stat, void *d_dz, int backward, void *cuda_stream) {
     if (!d || !d_z || !d_teacher || !d_index) return SGS_EINVAL;
     if (d->rows <= 0 || d->classes <= 0 || d->top <= 0 || d->top > DISTILL_TOP_MAX || !is_dtype(d->dtype) || !(d->temperature > 0.f) ||
-        !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature) || !std::isfinite(d->grad_scale))
+        !std::isfinite(d->temperature) || !std::isfinite(1.5f / d->temperature) || !std::isfinite(d->grad_scale))  // (1 / T times log2 e)
         return SGS_EINVAL;
     DistillArgs a;
     if (!pitch(d->ldz, d->classes, d->classes, &a.ldz) || !pitch(d->lddz, d->classes, d->classes, &a.lddz) || !pitch(d->ldt, d->top, d->top, &a.ldt)) return SGS_EINVAL;
@@ -3062,7 +3062,7 @@ sgs_status_t sgs_subnet_divergence(sgs_supernet_t *net, const sgs_subnet_cfg_t *
     if (!net) return SGS_EINVAL;
     if (!teacher || !subnets || n_subnets < 1 || !d_input || !divergence || batch <= 0 || res < 8 || res > 1024) return fail(net, SGS_EINVAL, "bad argument");
     const int classes = net->def.classes;
-    if (top < 1 || top > classes || top > TOP_LOGITS_MAX || !(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
+    if (top < 1 || top > classes || top > TOP_LOGITS_MAX || !(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.5f / temperature))
         return fail(net, SGS_EINVAL, "top or temperature out of range");
     if (!cfg_valid(net, teacher)) return fail(net, SGS_ECONFIG, "teacher: config outside the elastic sets");
     for (int i = 0; i < n_subnets; i++)

@@ -66,7 +66,7 @@ template <typename T> __device__ __forceinline__ Split split_row(const T *row, i
 }
 
 // Calls f(vector, its number) for this thread's vectors first + t, first + t + TEAM ...  Copies into a ring of the thread's own places in
-// shared memory run STREAM_AHEAD vectors ahead: enough bytes under way for HBM's latency (two blocks of 512 threads: 128 KB an SM), which
+// shared memory run six to eight vectors ahead: enough bytes under way for HBM's latency (two blocks of 512 threads: 128 KB an SM), which
 // registers do not hold, and nothing to wait for but the thread's own copies.
 constexpr int STREAM_STAGES = 4, STREAM_PAIR = 2, STREAM_RING = STREAM_STAGES * STREAM_PAIR;  // stages of two vectors
 template <bool LAST_USE> __device__ __forceinline__ void copy16(uint32_t dst, const uint4 *src, uint64_t policy) {  // LAST_USE: with an L2 policy
@@ -132,8 +132,8 @@ int parts_for(long long rows, double row_bytes, double least) {
 // that no two words are equal, larger values come first and of equal values (-0 and 0 are) the lower index.  NaN is the largest.
 //
 // A row (or part) in two passes: the k-th largest of the threads' own maxima bounds the k-th largest logit from below, and few more
-// than k logits reach it; these are collected, from the parts of the threads whose maximum does, and ranked by counting.  Rows where too many reach it (many equal values) find the
-// k-th largest word eight bits at a time.
+// than k logits reach it; these are collected, from the threads whose maximum does, and ranked by counting.  Rows where too many reach
+// it (many equal values) find the k-th largest word eight bits at a time.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);  // (-0 becomes 0)
@@ -171,13 +171,13 @@ struct TopParams {
 };
 
 template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) top_logits_kernel(const TopParams p) {
-    constexpr int N = Vec<T>::N, U = 4;
+    constexpr int N = Vec<T>::N;
     extern __shared__ uint4 ring[];
     uint64_t *joined = reinterpret_cast<uint64_t *>(ring);  // block 0, when the row has been read: the parts' words
     __shared__ uint64_t cand[TOP_CAP];
     __shared__ int n_cand, n_hot, want_s, hot[THREADS];
     __shared__ uint2 range[THREADS / 32];
-    __shared__ uint64_t prefix_s;
+    __shared__ uint32_t prefix_s;
     __shared__ int hist[256];
     const int t = threadIdx.x, part = (int)blockIdx.z, k = p.k;
     pdl_launch_dependents();
@@ -240,7 +240,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
     __syncthreads();
     auto take = [&](float v, uint32_t i) {
         const uint32_t key = key_of(v);
-        if (key >= least) {
+        if (key >= least && *(volatile int *)&n_cand <= TOP_CAP) {  // (more than enough are counted no further)
             const int at = atomicAdd(&n_cand, 1);  // (any order: the ranks below do not depend on it)
             if (at < TOP_CAP) cand[at] = (uint64_t)key << 32 | (uint32_t)~i;
         }
@@ -270,25 +270,29 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
     }
     __syncthreads();
     int n = n_cand;
-    if (n > TOP_CAP) {
-        // The k-th largest word itself.
-        uint64_t prefix = 0;
-        int want = k;
-        for (int shift = 56; shift >= 0; shift -= 8) {
+    // (Ranks cost the square, the way below some passes over the row: of 1000 zeros it takes 37 us for 512 rows and k = 64, ranking them all 151.)
+    if (n > (brief ? min(TOP_CAP, 2 * k + 256) : TOP_CAP)) {
+        // The k-th largest key itself, eight bits at a time; then the larger ones in any order and as many of its equals as are wanted, by
+        // their index.
+        constexpr int LOW = sizeof(T) == 2 ? 16 : 0;  // (a bf16's key has its lower half from its sign)
+        uint32_t prefix = 0;
+        int want = k;  // of the keys that begin with prefix
+        for (int shift = 24; shift >= LOW; shift -= 8) {
             for (int i = t; i < 256; i += THREADS) hist[i] = 0;
             __syncthreads();
-            // (runs of one digit, which is what brings rows here, are added up by the thread that meets them)
-            int held = -1, count = 0;
-            auto tally = [&](float v, uint32_t i) {
-                const uint64_t w = word_of(v, i);
-                if (shift < 56 && (w >> (shift + 8)) != (prefix >> (shift + 8))) return;
-                const int d = (int)(w >> shift) & 255;
-                if (d != held) {
-                    if (count) atomicAdd(&hist[held], count);
-                    held = d;
-                    count = 0;
+            // (rows come here for values that repeat: the thread keeps the counts of its last two digits)
+            int d0 = -1, n0 = 0, d1 = -1, n1 = 0;
+            auto tally = [&](float v, uint32_t) {
+                const uint32_t key = key_of(v);
+                if (shift < 24 && (key >> (shift + 8)) != (prefix >> (shift + 8))) return;
+                const int d = (int)(key >> shift) & 255;
+                if (d == d0) n0++;
+                else if (d == d1) n1++;
+                else {
+                    if (n1) atomicAdd(&hist[d1], n1);
+                    d1 = d0; n1 = n0;
+                    d0 = d; n0 = 1;
                 }
-                count++;
             };
             if (brief) each(tally);
             else
@@ -298,12 +302,13 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
 #pragma unroll
                     for (int j = 0; j < N; j++) tally(v[j], i + j);
                 }, tally);
-            if (count) atomicAdd(&hist[held], count);
+            if (n0) atomicAdd(&hist[d0], n0);
+            if (n1) atomicAdd(&hist[d1], n1);
             __syncthreads();
             if (t == 0) {
                 int d = 255, left = want;
                 while (d > 0 && hist[d] < left) left -= hist[d--];
-                prefix_s = prefix | (uint64_t)d << shift;
+                prefix_s = prefix | (uint32_t)d << shift;
                 want_s = left;
             }
             __syncthreads();
@@ -313,20 +318,38 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         if (t == 0) n_cand = 0;
         __syncthreads();
         auto keep = [&](float v, uint32_t i) {
-            const uint64_t w = word_of(v, i);
-            if (w >= prefix) cand[atomicAdd(&n_cand, 1)] = w;  // (exactly k of them)
+            if (key_of(v) >> LOW > prefix >> LOW) cand[atomicAdd(&n_cand, 1)] = word_of(v, i);  // (k - want of them)
         };
         if (brief) each(keep);
         else
             walk([&](const uint4 &q, uint32_t i) {
-                if (key_of(vec_max(q, (const T *)nullptr)) < (uint32_t)(prefix >> 32)) return;
+                if (key_of(vec_max(q, (const T *)nullptr)) >> LOW <= prefix >> LOW) return;
                 float v[N];
                 unpack(q, v);
 #pragma unroll
                 for (int j = 0; j < N; j++) keep(v[j], i + j);
             }, keep);
+        // this block's elements in the order of their index: its share of the head, its vectors, its share of the rest
+        const long long head = part == 0 ? s.head : 0, middle = head + (long long)(s.last - s.first) * N, all = middle + (part == 0 ? p.V - s.tail : 0);
+        int found = 0;
+        for (long long j0 = 0; j0 < all && found < want; j0 += THREADS) {
+            const long long j = j0 + t, i = j < head ? j : j < middle ? s.head + (long long)s.first * N + (j - head) : s.tail + (j - middle);
+            const float v = j < all ? to_float(ld_act(row + i)) : 0.f;
+            const bool same = j < all && key_of(v) >> LOW == prefix >> LOW;
+            const unsigned lanes = __ballot_sync(0xffffffffu, same);
+            __syncthreads();  // (the last round's counts have been read)
+            if ((t & 31) == 0) hist[t >> 5] = __popc(lanes);
+            __syncthreads();
+            int at = found + __popc(lanes & ((1u << (t & 31)) - 1));
+#pragma unroll
+            for (int w = 0; w < THREADS / 32; w++) {
+                if (w < t >> 5) at += hist[w];
+                found += hist[w];
+            }
+            if (same && at < want) cand[k - want + at] = word_of(v, (uint32_t)i);
+        }
         __syncthreads();
-        n = n_cand;
+        n = k;
     }
     float *values = p.values + (long long)blockIdx.x * p.ldt;
     int *index = p.index + (long long)blockIdx.x * p.ldt;
@@ -430,7 +453,7 @@ struct DisParams {
     float inv_t, temperature, grad_scale;
 };
 
-// A team of TEAM threads takes a row (or a cluster's part of one): a block, or for short rows a warp, four to a block.
+// A team of TEAM threads takes a row (or a cluster's part of one): a block, or for short rows a warp, eight to a block.
 //
 // What costs time besides the bytes is the chain of one row: list, row, two reductions, gradient.  So the list and the row's scale are
 // asked for before the row is streamed and looked at behind it, the loss is summed behind the gradient, and the sums over slots that name
