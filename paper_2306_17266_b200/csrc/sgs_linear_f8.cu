@@ -579,14 +579,27 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
             for (int j = 0; j < N; j++) put(j, j & 1 ? acc[j / 2].y : acc[j / 2].x);
         } else {
             const int rows = min(N, p.M - n0);
-            for (int n = part; n < rows; n += q.parts) {
-                float v = 0.f;
-                for (int s = 0; s < q.parts; s++) {
-                    float t;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(t) : "r"(block_addr(ring + (uint32_t)(n * TILE_M + l) * 4, (uint32_t)s)) : "memory");
-                    v += t;
+            // (all parts of four rows are asked for before the first is used: one by one, 64 rows took 64 ways to another SM)
+            constexpr int BATCH = 4;
+            for (int n = part; n < rows; n += BATCH * q.parts) {
+                float v[BATCH][8];
+#pragma unroll
+                for (int s = 0; s < 8; s++) {
+                    const uint32_t at = block_addr(ring + (uint32_t)l * 4, (uint32_t)min(s, q.parts - 1));
+#pragma unroll
+                    for (int i = 0; i < BATCH; i++) {
+                        v[i][s] = 0.f;
+                        if (s < q.parts && n + i * q.parts < rows)
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i][s]) : "r"(at + (uint32_t)((n + i * q.parts) * TILE_M) * 4) : "memory");
+                    }
                 }
-                put(n, v);
+#pragma unroll
+                for (int i = 0; i < BATCH; i++) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int s = 0; s < 8; s++) sum += v[i][s];
+                    if (n + i * q.parts < rows) put(n + i * q.parts, sum);
+                }
             }
         }
     }
