@@ -6,8 +6,8 @@
 // tensor memory and be added up in registers: acc += (sx * sw) * t, in fp32.  Slices are extents of the tensor maps: the first K
 // rows and C columns of the stored weights, zeros beyond.
 //
-// Three forms, by the size of the call: pairs of blocks on tiles of 256 x 256 where those fill the GPU, single blocks on tiles of 128 x 128,
-// and for up to 64 rows, or fewer tiles than SMs, tiles of 128 rows of w whose reduction a cluster shares.
+// Three forms, by the size of the call (the rule stands at the launch): pairs of blocks on tiles of 256 x 256, single blocks on tiles of
+// 128 x 128, and for few rows, or few tiles and a long reduction, tiles of 128 rows of w whose reduction a cluster shares.
 //
 // What bounds the large form (8192^3, 585 us, 1.88 PFLOP/s at some 1.55 GHz under the power cap): the way of a block's sums through the
 // warps.  The MMAs of a block take 512 clocks; with the sums left out a block takes 745 (operand copies and MMAs share the port of shared
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
 
 // Few rows of x: the rows of w take the lanes (128 a block), up to N rows of x the columns, and the blocks of a cluster share the
 // reduction, whose parts meet in distributed shared memory, in the order of c.  What bounds such a call is w's bytes: 16 KB of them a
-// stage, two thread blocks an SM (one row, 8192 filters, 4096 channels: 9.3 us, 3.6 TB/s; 16384 x 8192: 57 % of the DRAM rate; the rest is
+// stage, two thread blocks an SM (one row, 8192 filters, 4096 channels: 9.2 us, 3.6 TB/s; 16384 x 8192: 57 % of the DRAM rate; the rest is
 // the way in and out: launch, first copies, the cluster's two meetings).  Blocks that share an SM hold 256 columns of tensor memory at most
 // each, and kernels that fit beside them the rest: no allocation waits for another block's, which a cluster whose blocks wait for each
 // other could not afford.  Warp 0 loads, 1 issues, 2 brings the scales, warps 4..7 add up, a quadrant of the lanes each.
@@ -553,53 +553,72 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_s
                 if ((i ^= 1) == 0) sc_phase ^= 1;
             }
         }
-        // the parts' sums: [row of x][lane], in the operand stages (all of this block's MMAs have read theirs)
-        if (q.parts > 1 && ok) {
+        // the sums: [row of x][lane], in the operand stages (all of this block's MMAs have read theirs)
+        if (ok) {
             float *sums = reinterpret_cast<float *>(smem) + l;
 #pragma unroll
             for (int j = 0; j < N; j++) sums[j * TILE_M] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
         }
+        if (q.parts == 1) asm volatile("bar.sync 1, 128;" ::: "memory");
     }
-    const bool finisher = warp >= 4;
     if (q.parts > 1) pair_sync();  // (every thread of every block of the cluster)
-    if (finisher && !*abort_flag) {
-        const int l = (warp & 3) * 32 + lane, f = f0 + l;
-        const float bias = p.bias && f < p.K ? ld_act(p.bias + f) : 0.f;
-        auto put = [&](int n, float v) {
-            if (f >= p.K || n0 + n >= p.M) return;
-            v += bias;
-            if (p.act == ACT_RELU) v = v < 0.f ? 0.f : v;
-            else if (p.act == ACT_HSWISH) v = act_fn(v, ACT_HSWISH);
+    // A warp takes a row, a lane four features.  (One feature a lane and its columns written out, 64 stores behind their branches were read
+    // once each from a cold instruction cache: 64 x 320 x 360 took 9.1 us, 5.5 so.)
+    if (warp >= 4 && !*abort_flag) {
+        const int f = f0 + lane * 4, rows = min(N, p.M - n0), size = p.y_bf16 ? 2 : 4;
+        const bool whole = f + 4 <= p.K && ((reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)(p.ldy * size)) & (uintptr_t)(4 * size - 1)) == 0;
+        float bias[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) bias[i] = p.bias && f + i < p.K ? ld_act(p.bias + f + i) : 0.f;
+        auto put = [&](int n, const float (&sum)[4]) {
+            float o[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                o[i] = sum[i] + bias[i];
+                if (p.act == ACT_RELU) o[i] = o[i] < 0.f ? 0.f : o[i];
+                else if (p.act == ACT_HSWISH) o[i] = act_fn(o[i], ACT_HSWISH);
+            }
             const long long at = (long long)(n0 + n) * p.ldy + f;
-            if (p.y_bf16) static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
-            else static_cast<float *>(p.y)[at] = v;
+            if (p.y_bf16) {
+                __nv_bfloat16 *y = static_cast<__nv_bfloat16 *>(p.y) + at;
+                __nv_bfloat162 h[2] = {__floats2bfloat162_rn(o[0], o[1]), __floats2bfloat162_rn(o[2], o[3])};
+                if (whole) *reinterpret_cast<uint2 *>(y) = *reinterpret_cast<uint2 *>(h);
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (f + i < p.K) y[i] = __float2bfloat16_rn(o[i]);
+            } else {
+                float *y = static_cast<float *>(p.y) + at;
+                if (whole) *reinterpret_cast<float4 *>(y) = make_float4(o[0], o[1], o[2], o[3]);
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (f + i < p.K) y[i] = o[i];
+            }
         };
         if (q.parts == 1) {
-#pragma unroll
-            for (int j = 0; j < N; j++) put(j, j & 1 ? acc[j / 2].y : acc[j / 2].x);
+            const float4 *sums = reinterpret_cast<const float4 *>(smem) + lane;
+#pragma unroll 4
+            for (int n = warp - 4; n < rows; n += 4) {
+                const float4 v = sums[n * (TILE_M / 4)];
+                put(n, {v.x, v.y, v.z, v.w});
+            }
         } else {
-            const int rows = min(N, p.M - n0);
-            // (all parts of four rows are asked for before the first is used: one by one, 64 rows took 64 ways to another SM)
-            constexpr int BATCH = 4;
-            for (int n = part; n < rows; n += BATCH * q.parts) {
-                float v[BATCH][8];
+#pragma unroll 1
+            for (int n = part + (warp - 4) * q.parts; n < rows; n += 4 * q.parts) {
+                float v[8][4], sum[4] = {0.f, 0.f, 0.f, 0.f};  // all parts are asked for before the first is used
 #pragma unroll
-                for (int s = 0; s < 8; s++) {
-                    const uint32_t at = block_addr(ring + (uint32_t)l * 4, (uint32_t)min(s, q.parts - 1));
+                for (int s = 0; s < 8; s++)
+                    if (s < q.parts)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                     : "=f"(v[s][0]), "=f"(v[s][1]), "=f"(v[s][2]), "=f"(v[s][3])
+                                     : "r"(block_addr(ring + (uint32_t)(n * TILE_M + lane * 4) * 4, (uint32_t)s)) : "memory");
+                    else v[s][0] = v[s][1] = v[s][2] = v[s][3] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < BATCH; i++) {
-                        v[i][s] = 0.f;
-                        if (s < q.parts && n + i * q.parts < rows)
-                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i][s]) : "r"(at + (uint32_t)((n + i * q.parts) * TILE_M) * 4) : "memory");
-                    }
-                }
+                for (int s = 0; s < 8; s++)
 #pragma unroll
-                for (int i = 0; i < BATCH; i++) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int s = 0; s < 8; s++) sum += v[i][s];
-                    if (n + i * q.parts < rows) put(n + i * q.parts, sum);
-                }
+                    for (int i = 0; i < 4; i++) sum[i] += v[s][i];
+                put(n, sum);
             }
         }
     }
@@ -625,7 +644,7 @@ template <int N, bool W_ROWS> cudaError_t launch_split(F8Params &p, const Linear
     const unsigned filters = (unsigned)((a.K + TILE_M - 1) / TILE_M), rows = (unsigned)((a.M + N - 1) / N);
     F8Split q;
     q.parts = 1;
-    // (one row, 8192 x 4096: 9.3 us with 4 parts, 10.0 with 2, 12.8 with 8)
+    // (one row, 8192 x 4096: 9.2 us with 4 parts, 10.0 with 2, 12.8 with 8)
     while (q.parts < 8 && (long long)filters * rows * q.parts < sm_count() && p.blocks >= 4 * q.parts) q.parts *= 2;
     q.part_blocks = (p.blocks + q.parts - 1) / q.parts;
     while ((q.parts - 1) * q.part_blocks >= p.blocks) q.parts--;  // (no block without a share; any number makes a cluster)
@@ -674,11 +693,18 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
         p.bulk_y = a.K / unit * unit;
     p.formats = ((uint32_t)(a.x_e5m2 ? 1 : 0) << 7) | ((uint32_t)(a.w_e5m2 ? 1 : 0) << 10);
     const long long tiles = (long long)((a.M + 127) / 128) * ((a.K + 127) / 128);
-    // (layers with fewer tiles than SMs: 128 x 4096 x 4096 takes 15 us split, 28 in tiles of 128 x 128 on 32 SMs)
+    // Few rows split the reduction over clusters.  So do more than 32 where the tiles of 128 x 128 would leave three SMs in four idle and the
+    // reduction is long enough to pay for the meeting (split and in tiles, us: 128 x 4096 x 4096 11.1 and 13.3, 300 x 1000 x 8192 12.1 and
+    // 21.8; 256 x 4096 x 4096, 64 tiles, 15.5 and 13.6; 128 x 4096 x 1024 7.0 and 6.0, 64 x 320 x 640 6.5 and 5.0).
     if (a.M <= 16) return a.w_rows ? launch_split<16, true>(p, a, g_set[4], st) : launch_split<16, false>(p, a, g_set[5], st);
     if (a.M <= 32) return a.w_rows ? launch_split<32, true>(p, a, g_set[6], st) : launch_split<32, false>(p, a, g_set[7], st);
-    if (a.M <= 64 || tiles < sm_count()) return a.w_rows ? launch_split<64, true>(p, a, g_set[8], st) : launch_split<64, false>(p, a, g_set[9], st);
-    const bool pairs = (long long)((a.M + 255) / 256) * ((a.K + 255) / 256) * 2 >= sm_count();
+    if (tiles * 4 <= sm_count() && p.blocks > 8) return a.w_rows ? launch_split<64, true>(p, a, g_set[8], st) : launch_split<64, false>(p, a, g_set[9], st);
+    // Pairs of SMs take a tile of 256 x 256 in 1.6 times the time that one takes for 128 x 128 (4096 long: 16.5 us more for each wave, and
+    // 10.2): they win where they need that many fewer waves.  1024 x 4096, one wave and two, 22.5 and 24.5 us; 1280 x 4096, two and three,
+    // 38.7 and 33.6; 512 x 4096, one and one, 21.4 and 14.2; 50176 x 64, 256 long, three and three, 11.6 and 9.0.
+    const long long sms = sm_count(), pair_tiles = (long long)((a.M + 255) / 256) * ((a.K + 255) / 256);
+    const long long waves = (tiles + sms - 1) / sms, pair_waves = (pair_tiles + sms / 2 - 1) / (sms / 2);
+    const bool pairs = 8 * pair_waves <= 5 * waves;
     if (a.w_rows) return pairs ? launch_tiles<2, 256, true>(p, a, g_set[0], st) : launch_tiles<1, 128, true>(p, a, g_set[1], st);
     return pairs ? launch_tiles<2, 256, false>(p, a, g_set[2], st) : launch_tiles<1, 128, false>(p, a, g_set[3], st);
 }
