@@ -84,6 +84,21 @@ def test_linear_output_that_starts_anywhere(M):
             assert (err <= f8_ref.linear_tolerance(ref, size, C, 0, bf16)).all()
 
 
+@pytest.mark.parametrize("w_block", [1, 128])
+@pytest.mark.parametrize("M,K,C", [(64, 203, 1200), (33, 1000, 8192), (200, 201, 1300), (300, 130, 4100), (129, 1100, 2100), (64, 4700, 1100), (16, 9, 9000)])
+def test_linear_reduction_shared_by_a_cluster(M, K, C, w_block):
+    # two to eight blocks share it, the last with fewer of its blocks or none to spare; rows of the output that do not start on four elements
+    run_linear(None, M, K, C, K, C, w_block=w_block, y="f32", act=2, seed=K)
+    run_linear(None, M, K, C, K + 5, C + 40, w_block=w_block, y="bf16", ldy=K + 3, ldsx=M + 1, ldsw=K + 9 if w_block == 1 else 60, seed=C)
+    run_linear(None, M, K, C, K, C, w_block=w_block, y="bf16", act=1, bias=False, ldy=(K + 7) // 4 * 4, seed=C)
+
+
+@pytest.mark.parametrize("M,K,C", [(64, 320, 640), (129, 300, 1024), (600, 1030, 1200), (1100, 4000, 1200), (1290, 4090, 300)])
+def test_linear_either_side_of_the_choice_of_form(M, K, C):
+    run_linear(None, M, K, C, K, C, y="bf16", act=1, seed=M)
+    run_linear(None, M, K, C, K, C, w_block=1, y="f32", seed=M)
+
+
 def test_offsets_beyond_32_bits():
     # a few rows far apart: element offsets up to 2.4e9
     pitch, M, V = 1 << 28, 10, 3000
