@@ -297,6 +297,14 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                 const float f = rs[0];
                 rs[0] = rs[1]; rs[1] = rs[2]; rs[2] = rs[3];
                 const float2 s2 = make_float2(f, f);
+                // the columns' scales, four loads of shared memory ahead in the pairs' kernel (4096 x 2048 over 8197, us: 109.5, one by one
+                // 114.3, eight ahead spill, 130; single blocks, 512 x 4096 x 4096: 20.1 ahead, 19.6 one by one)
+                constexpr bool EARLY = W_ROWS && CTAS == 2;
+                float4 c[4];
+                if (EARLY) {
+#pragma unroll
+                    for (int t = 0; t < 4; t++) c[t] = *reinterpret_cast<const float4 *>(cs + 4 * t);
+                }
 #pragma unroll
                 for (int j0 = 0; j0 < COLS; j0 += 32) {
                     uint32_t (&w)[32] = v[(j0 / 32) & 1], (&next)[32] = v[(j0 / 32 + 1) & 1];
@@ -320,9 +328,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                     for (int j = 0; j < 16; j += 2) {
                         float2 g0 = s2, g1 = s2;
                         if (W_ROWS) {
-                            const float4 c = *reinterpret_cast<const float4 *>(cs + j0 + 2 * j);
-                            g0 = __fmul2_rn(s2, make_float2(c.x, c.y));
-                            g1 = __fmul2_rn(s2, make_float2(c.z, c.w));
+                            const float4 e = EARLY ? c[j / 2 % 4] : *reinterpret_cast<const float4 *>(cs + j0 + 2 * j);
+                            if (EARLY && j0 + 2 * j + 16 < COLS) c[j / 2 % 4] = *reinterpret_cast<const float4 *>(cs + j0 + 2 * j + 16);
+                            g0 = __fmul2_rn(s2, make_float2(e.x, e.y));
+                            g1 = __fmul2_rn(s2, make_float2(e.z, e.w));
                         }
                         acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1])), g0, acc[j0 / 2 + j]);
                         acc[j0 / 2 + j + 1] = __ffma2_rn(make_float2(__uint_as_float(w[2 * j + 2]), __uint_as_float(w[2 * j + 3])), g1, acc[j0 / 2 + j + 1]);
