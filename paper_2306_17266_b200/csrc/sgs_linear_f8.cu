@@ -703,7 +703,7 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
     p.formats = ((uint32_t)(a.x_e5m2 ? 1 : 0) << 7) | ((uint32_t)(a.w_e5m2 ? 1 : 0) << 10);
     const long long tiles = (long long)((a.M + 127) / 128) * ((a.K + 127) / 128);
     // Few rows split the reduction over clusters.  So do more than 32 where the tiles of 128 x 128 would leave three SMs in four idle and the
-    // reduction is long enough to pay for the meeting (split and in tiles, us: 128 x 4096 x 4096 11.1 and 13.3, 300 x 1000 x 8192 12.1 and
+    // reduction is long enough to pay for the meeting (split and in tiles, us: 128 x 4096 x 4096 11.1 and 13.3, 300 x 1000 x 8192 14.0 and
     // 21.8; 256 x 4096 x 4096, 64 tiles, 15.5 and 13.6; 128 x 4096 x 1024 7.0 and 6.0, 64 x 320 x 640 6.5 and 5.0).
     if (a.M <= 16) return a.w_rows ? launch_split<16, true>(p, a, g_set[4], st) : launch_split<16, false>(p, a, g_set[5], st);
     if (a.M <= 32) return a.w_rows ? launch_split<32, true>(p, a, g_set[6], st) : launch_split<32, false>(p, a, g_set[7], st);
