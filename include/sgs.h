@@ -530,9 +530,9 @@ sgs_status_t sgs_distill(const sgs_distill_desc_t *desc, const void *d_z, const 
                          float *d_loss, float *d_stat, void *d_dz, void *cuda_stream);
 sgs_status_t sgs_distill_backward(const sgs_distill_desc_t *desc, const void *d_z, const float *d_teacher, const int *d_index,
                                   const float *d_stat, const float *d_row_scale, void *d_dz, void *cuda_stream);
-/* The five calls above are asynchronous on `cuda_stream`, allocate nothing, keep nothing between calls and can be captured after a
- * first call outside the capture (sgs_linear_f8; the others at once).  Everything passed in may be what earlier work on the stream
- * writes; outputs must not overlap inputs (but for dz = z).  Pointers are of the current device (SGS_EINVAL for another device's
+/* The five calls above are asynchronous on `cuda_stream`, allocate nothing, keep nothing between calls and can be captured, sgs_linear_f8
+ * after a first call outside the capture (until then it refuses with SGS_EINVAL).  Everything passed in may be what earlier work on the
+ * stream writes; outputs must not overlap inputs (but for dz = z).  Pointers are of the current device (SGS_EINVAL for another device's
  * and for host memory that the device cannot read). */
 
 /*

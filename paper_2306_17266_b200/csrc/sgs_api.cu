@@ -3004,7 +3004,9 @@ sgs_status_t sgs_linear_f8(const sgs_linear_f8_desc_t *d, const void *d_x, const
     if (!on_current_device({d_x, d_sx, d_w, d_sw, d_bias, d_y})) return SGS_EINVAL;
     int dev = 0;
     if (!tc_available()) return SGS_EUNSUPPORTED;
-    if (cudaGetDevice(&dev) != cudaSuccess || tc_conv_init(dev) != cudaSuccess) return SGS_ECUDA;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SGS_ECUDA;
+    if (!tc_status_word(dev) && being_captured((cudaStream_t)cuda_stream)) return SGS_EINVAL;  // (the first call allocates the status word, which would end the capture)
+    if (tc_conv_init(dev) != cudaSuccess) return SGS_ECUDA;
     a.x = d_x; a.w = d_w; a.sx = d_sx; a.sw = d_sw; a.bias = d_bias; a.y = d_y;
     a.M = d->M; a.K = d->K; a.C = d->C; a.x_e5m2 = d->x_format == SGS_E5M2; a.w_e5m2 = d->w_format == SGS_E5M2;
     a.y_bf16 = d->y_dtype == SGS_BF16; a.act = d->act;

@@ -1,5 +1,7 @@
 """Edges of the 8-bit float layers and of the operators on logits: the forms that many rows take, several tiles a block, outputs that start
 anywhere, offsets beyond 32 bits, host threads."""
+import subprocess
+import sys
 import threading
 
 import numpy as np
@@ -165,3 +167,41 @@ def test_host_threads_with_streams_of_their_own():
     for r in results[1:]:
         for a, b in zip(results[0], r):
             assert torch.equal(a, b)
+
+
+FIRST_CALL_CAPTURED = """
+import torch
+import paper_2306_17266_b200 as sgs
+x = torch.full((16, 128), 0x38, dtype=torch.uint8, device="cuda")  # ones
+s = torch.ones((1, 16), device="cuda")
+y = torch.zeros((16, 16), device="cuda")
+d = sgs.LinearF8Desc(M=16, K=16, C=128, Kmax=16, Cmax=128, w_block_rows=1, y_dtype=sgs.SGS_F32)
+call = lambda st: sgs.linear_f8(d, x.data_ptr(), s.data_ptr(), x.data_ptr(), s.data_ptr(), 0, y.data_ptr(), st.cuda_stream)
+st, other, graph = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph, stream=st):
+    y.add_(1)
+    try:
+        call(st)
+        raise SystemExit("not refused")
+    except sgs.SgsError as e:
+        assert e.status == sgs.binding.SGS_EINVAL, e.status
+graph.replay()
+torch.cuda.synchronize()
+assert (y == 1).all()
+call(other)
+torch.cuda.synchronize()
+assert (y == 128).all()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph, stream=st):
+    call(st)
+y.zero_()
+graph.replay()
+torch.cuda.synchronize()
+assert (y == 128).all() and sgs.device_status() == 0
+"""
+
+
+def test_first_layer_call_under_capture_is_refused_and_the_capture_goes_on():
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL_CAPTURED], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
