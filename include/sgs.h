@@ -513,7 +513,8 @@ sgs_status_t sgs_top_logits(const sgs_top_logits_desc_t *desc, const void *d_z, 
  * probabilities.  Logits of minus infinity have q = 0 (a row of nothing else: q = 0 everywhere); with g = 0 a row's gradient is 0.
  * NaN goes through.  All sums are fp32, in an order that depends on sizes, types, pitches and alignment alone; dz is rounded once.
  *   d_z [rows][ldz] and d_dz [rows][lddz] of dtype     d_teacher fp32, d_index int32 [rows][ldt]     d_row_scale fp32 [rows] or NULL (1)
- *   d_loss fp32 [rows]     d_stat fp32 [rows][2] or NULL: the row's largest logit and log sum exp((z - largest) / T)
+ *   d_loss fp32 [rows]     d_stat fp32 [rows][2] or NULL: the row's largest logit and log sum exp((z - largest) / T) (in a row
+ *   with a NaN both are NaN, or with plus infinity beside it that and NaN)
  *   d_dz NULL: the loss alone.  d_dz may be d_z with the same pitch (the gradient replaces the logits).
  * sgs_distill_backward - dz alone, from the statistics that sgs_distill left; T, lists and logits as then.
  * 1 <= top <= SGS_DISTILL_TOP_MAX, 0 < T < infinity and 1.5 / T finite, grad_scale finite.

@@ -563,8 +563,11 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
         stud = warp_join(stud, a);
         cluster_arrive();  // (nobody leaves before all have read: the wait is at the end)
     }
-    const float zmax = p.backward ? kept.x : stud.x, logsum = p.backward ? kept.y : logf(stud.y);
-    const float base = zmax == NEG_INF ? 0.f : zmax, off = zmax == NEG_INF ? 0.f : logsum;
+    // The running maximum leaves NaN out, the sum does not: a row whose sum is NaN has a NaN (or plus infinity) among its logits.  A row is
+    // empty where its sum is 0, not where the largest of its numbers is minus infinity: beside that there may be a NaN.
+    const float logsum = p.backward ? kept.y : logf(stud.y);
+    const float zmax = p.backward ? kept.x : logsum == logsum || stud.x == -NEG_INF ? stud.x : logsum;
+    const float base = zmax == NEG_INF ? 0.f : zmax, off = logsum == NEG_INF ? 0.f : logsum;
     const float tmax = teach.x == NEG_INF ? 0.f : teach.x, tsum = teach.y;
     const float c = used ? p.grad_scale * p.temperature * row_scale : 0.f, off2 = off * LOG2E;
     float loss = 0.f;
