@@ -450,7 +450,8 @@ struct DisParams {
     float *loss, *stat;
     int V, k, backward, parts, table;  // table: places of the table of classes, a power of two
     long long ldz, lddz, ldt;
-    float inv_t, temperature, grad_scale;
+    float inv_t, temperature;
+    double grad_factor;  // grad_scale * temperature: in 64 bits, since it may leave fp32's range where its product with a row's scale does not
 };
 
 // A team of TEAM threads takes a row (or a cluster's part of one): a block, or for short rows a warp, eight to a block.
@@ -569,7 +570,7 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
     const float zmax = p.backward ? kept.x : logsum == logsum || stud.x == -NEG_INF ? stud.x : logsum;
     const float base = zmax == NEG_INF ? 0.f : zmax, off = logsum == NEG_INF ? 0.f : logsum;
     const float tmax = teach.x == NEG_INF ? 0.f : teach.x, tsum = teach.y;
-    const float c = used ? p.grad_scale * p.temperature * row_scale : 0.f, off2 = off * LOG2E;
+    const float c = used ? (float)(p.grad_factor * (double)row_scale) : 0.f, off2 = off * LOG2E;
     float loss = 0.f;
     const float log_tsum = logf(tsum);
 #pragma unroll
@@ -708,7 +709,7 @@ cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
     DisParams p;
     p.z = a.z; p.dz = a.dz; p.teacher = a.teacher; p.row_scale = a.row_scale; p.index = a.index; p.loss = a.loss; p.stat = a.stat;
     p.V = a.classes; p.k = a.top; p.backward = a.backward; p.ldz = a.ldz; p.lddz = a.lddz; p.ldt = a.ldt;
-    p.inv_t = 1.f / a.temperature; p.temperature = a.temperature; p.grad_scale = a.grad_scale;
+    p.inv_t = 1.f / a.temperature; p.temperature = a.temperature; p.grad_factor = (double)a.grad_scale * a.temperature;
     const double bytes = (double)a.classes * (a.bf16 ? 2 : 4);
     p.parts = parts_for(a.rows, bytes, 16384);
     return a.bf16 ? launch_distill_type<__nv_bfloat16>(p, a.rows, bytes, st) : launch_distill_type<float>(p, a.rows, bytes, st);
