@@ -450,7 +450,7 @@ sgs_status_t sgs_aux_op(int n_members, const sgs_aux_desc_t *desc, const sgs_aux
  *   scale = 2^max(-126, ceil(log2(amax / FMAX))), amax the block's largest finite magnitude, FMAX 448 (e4m3) or 57344 (e5m2)
  *   code = nearest(x / scale), ties to even; NaN and infinities become NaN
  * d_q and d_scale, or d_qt and d_scale_t, may be NULL together.  Bytes of a row beyond its codes and scales beyond a line's are
- * left as they were.
+ * left as they were.  Rows or columns within 512 of 2^31, or more than 2^30 - 1 tiles of 128 x 128: SGS_EUNSUPPORTED.
  */
 typedef enum { SGS_E4M3 = 0, SGS_E5M2 = 1 } sgs_f8_format_t;
 typedef struct {
@@ -475,7 +475,8 @@ sgs_status_t sgs_quantize_f8(const sgs_quantize_f8_desc_t *desc, const void *d_x
  *   d_y [M][ldy] fp32 or bf16
  * The gradients of such a layer are layers of the same kind: with g the gradient of its sums, dx = g w takes g row-wise and w
  * transposed; dw = g^T x takes both transposed, x's with a scale per row (w_block_rows 1), and an fp32 y.
- * x and w 16-byte aligned with pitches in multiples of 16, else SGS_EUNSUPPORTED (likewise more than 2^31 - 1 tiles).
+ * x and w 16-byte aligned with pitches in multiples of 16, else SGS_EUNSUPPORTED (likewise more than 2^31 - 1 tiles, and M, K or C
+ * within 512 of 2^31).
  */
 typedef struct {
     int M, K, C;              /* rows of x; rows (filters) and columns (channels) of w in use */

@@ -2978,7 +2978,8 @@ sgs_status_t sgs_quantize_f8(const sgs_quantize_f8_desc_t *d, const void *d_x, v
         !pitch(d->lds, lines, lines, &a.lds) || !pitch(d->ldst, lines_t, lines_t, &a.ldst))
         return SGS_EINVAL;
     if (!aligned(d_x, d->dtype == SGS_BF16 ? 2 : 4) || !aligned(d_scale, 4) || !aligned(d_scale_t, 4)) return SGS_EINVAL;
-    if (2 * blocks128(d->rows) * blocks128(d->cols) > 2147483647ll) return SGS_EUNSUPPORTED;  // (blocks of a launch, of 64 rows at the least)
+    if (2 * blocks128(d->rows) * blocks128(d->cols) > 2147483647ll || d->rows > 2147483647 - 512 || d->cols > 2147483647 - 512)
+        return SGS_EUNSUPPORTED;  // (blocks of a launch, of 64 rows at the least; rows and columns of the last tile are counted in 32 bits)
     if (!on_current_device({d_x, d_q, d_scale, d_qt, d_scale_t})) return SGS_EINVAL;
     a.x = d_x; a.q = d_q; a.qt = d_qt; a.scale = d_scale; a.scale_t = d_scale_t;
     a.rows = d->rows; a.cols = d->cols; a.bf16 = d->dtype == SGS_BF16; a.e5m2 = d->format == SGS_E5M2;
