@@ -672,7 +672,7 @@ template <typename T> cudaError_t launch_distill_type(DisParams &p, int rows, do
     if (bytes <= 8192 && p.k <= 128 && rows >= 8 * sm_count()) {
         constexpr int TEAMS = 256 / 32;
         p.parts = 1;
-        return launch_distill_blocks<T, 32, 256>(p, dim3((unsigned)((rows + TEAMS - 1) / TEAMS)), TEAMS * list, rows, st);
+        return launch_distill_blocks<T, 32, 256>(p, dim3((unsigned)(((long long)rows + TEAMS - 1) / TEAMS)), TEAMS * list, rows, st);
     }
     // Blocks of 256 threads keep four rows of an SM at work, which serves the loss alone; with a gradient the rows between their two
     // passes have to stay in L2 together with what is written: blocks of 512, two rows an SM (2048 x 65536 bf16: 123 and 109 us; the loss
