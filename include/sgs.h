@@ -440,7 +440,7 @@ sgs_status_t sgs_aux_op(int n_members, const sgs_aux_desc_t *desc, const sgs_aux
  * gradients fit too).  A matrix of R rows and C columns is held as
  *   codes  [R][ld] bytes, e4m3 or e5m2, ld a multiple of 16 for the layers that read them
  *   scales fp32 [ceil(C / 128)][pitch]: a line for each block of 128 columns, in it a scale for every row, or for every 128 rows
- * and stands for code * scale.  The scales are any finite numbers; sgs_quantize_f8 writes powers of two.
+ * and stands for code * scale.  The scales are finite numbers of either sign; sgs_quantize_f8 writes powers of two, 2^-126 for zeros.
  *
  * sgs_quantize_f8 - codes and scales of a matrix x [rows][cols] (row-wise), of its transpose, or of both from one read:
  *   d_q [rows][ldq], d_scale [ceil(cols/128)][lds]       blocks of 1 x 128 elements (block_rows 1) or 128 x 128 (block_rows 128)
@@ -471,6 +471,8 @@ sgs_status_t sgs_quantize_f8(const sgs_quantize_f8_desc_t *desc, const void *d_x
  *   y[m][k] = act( sum_b sx[b][m] * sw[b][k / w_block_rows] * ( sum_{c in block b, c < C} x[m][c] * w[k][c] ) + bias[k] )
  * Sums are fp32: the products of a block in the tensor core, the blocks in registers, in the order of c within groups that the size
  * of the call alone decides.  y is rounded once.
+ * A block's two scales are multiplied first, in fp32: where their product is beyond 2^128 the block is infinite or NaN, where it is below
+ * 2^-126 it is rounded as numbers of that size are (to 0 below 2^-150), and the block with it.
  *   d_x [M][ldx], d_sx [ceil(C/128)][ldsx] a scale per row     d_w [Kmax][ldw], d_sw [ceil(C/128)][ldsw]     d_bias [>= K] fp32 or NULL
  *   d_y [M][ldy] fp32 or bf16
  * The gradients of such a layer are layers of the same kind: with g the gradient of its sums, dx = g w takes g row-wise and w
