@@ -190,14 +190,10 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         stream<THREADS, THREADS>(ring, vec, s.first, s.last, t, [&](const uint4 &q, int i) { f(q, (uint32_t)(s.head + i * N)); });
         if (t < s.edges) { const long long e = s.edge(t); f1(to_float(ld_act(row + e)), (uint32_t)e); }
     };
-    // Short parts, where vectors would leave threads without any logit: element by element.
-    const long long e0 = part == 0 ? 0 : s.head + (long long)s.first * N, e1 = part == p.parts - 1 ? p.V : s.head + (long long)s.last * N;
-    const bool brief = e1 - e0 <= 2 * N * THREADS;
-    const bool edges_apart = p.parts > 1;  // (then the edges are block 0's: the ranges above leave the tail to it)
+    // Short rows, where vectors would leave threads without any logit: element by element.  (A row that a cluster shares is never short.)
+    const bool brief = p.parts == 1 && p.V <= 2 * N * THREADS;
     auto each = [&](auto f1) {
-        const long long last = edges_apart ? s.head + (long long)s.last * N : p.V;
-        for (long long i = (edges_apart ? s.head + (long long)s.first * N : 0) + t; i < last; i += THREADS) f1(to_float(ld_act(row + i)), (uint32_t)i);
-        if (edges_apart && t < s.edges) { const long long e = s.edge(t); f1(to_float(ld_act(row + e)), (uint32_t)e); }
+        for (int i = t; i < p.V; i += THREADS) f1(to_float(ld_act(row + i)), (uint32_t)i);
     };
     uint32_t most = 0;  // largest key (0: below every key)
     int top_vec = -1;   // the vector that has it
