@@ -429,7 +429,8 @@ struct F8Split {
     int parts, part_blocks;  // blocks of a cluster; blocks of the reduction that each of them takes (the last may have fewer)
 };
 template <int N, bool W_ROWS>
-__global__ void __launch_bounds__(F8_SPLIT_THREADS, N <= 64 ? 2 : 1) linear_f8_split_kernel(const __grid_constant__ F8Params p, const F8Split q) {
+__global__ void __launch_bounds__(F8_SPLIT_THREADS, 2) linear_f8_split_kernel(const __grid_constant__ F8Params p, const F8Split q) {
+    static_assert(N <= 64, "two blocks an SM: registers, shared memory and 256 columns of tensor memory each");
     constexpr int STAGE = F8_A_BYTES + N * F8_BLOCK, STAGES = F8_SPLIT_RING / STAGE, NACC = N <= 32 ? 8 : 256 / N;
     struct Shared {
         alignas(16) float w_scale[2][W_ROWS ? TILE_M : 1][F8_AHEAD];
