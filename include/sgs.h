@@ -586,6 +586,12 @@ sgs_status_t sgs_debug_expire_wait(unsigned limit_us, void *cuda_stream);
  * ran out.  Sets the device status word. */
 sgs_status_t sgs_debug_expire_team_wait(int team, int block, int thread, unsigned limit_us, int *d_left, void *cuda_stream);
 
+/* The same for the 8-bit float layer: sgs_linear_f8, but the weights' block `block` of the reduction (0 .. ceil(C / 128) - 1) is never
+ * copied in, so that the waits for it run out after limit_us.  The kernel sets the device status word and returns; rows of y that it had
+ * not written by then are left as they were, or, where the blocks of a cluster share the reduction, may hold anything. */
+sgs_status_t sgs_debug_expire_f8_wait(const sgs_linear_f8_desc_t *desc, const void *d_x, const float *d_sx, const void *d_w, const float *d_sw,
+                                      const float *d_bias, void *d_y, int block, unsigned limit_us, void *cuda_stream);
+
 /* Test aid: how persistent execution with `team` (1, 2, 4, 8, 16) SMs a query cuts a pointwise layer of `pixels` x `filters` into tiles
  * of 128 pixels x *tile_filters (16 .. 256), *filter_tiles of them along the filters, and how many filters of tile i < max_tiles, its
  * first held[i], come out of a weight buffer that holds the layer's first `held_rows` filters. */

@@ -27,7 +27,7 @@ EXPORTS = [
     "sgs_set_option", "sgs_get_counter", "sgs_last_error", "sgs_supernet_free", "sgs_conv2d_sliced", "sgs_device_status",
     "sgs_profile_read", "sgs_conv2d_sliced_static", "sgs_cache_set_candidates", "sgs_cache_set_policy",
     "sgs_sched_create", "sgs_sched_free", "sgs_sched_dims", "sgs_sched_set_table", "sgs_sched_get_table", "sgs_sched_measure",
-    "sgs_sched_step", "sgs_sched_subnet", "sgs_profile_trace", "sgs_layer_name", "sgs_aux_op", "sgs_device_status_clear", "sgs_debug_expire_wait", "sgs_debug_expire_team_wait", "sgs_debug_pointwise_tiles", "sgs_debug_layer_map", "sgs_measure_fma_peak", "sgs_conv2d_sliced_i8",
+    "sgs_sched_step", "sgs_sched_subnet", "sgs_profile_trace", "sgs_layer_name", "sgs_aux_op", "sgs_device_status_clear", "sgs_debug_expire_wait", "sgs_debug_expire_team_wait", "sgs_debug_expire_f8_wait", "sgs_debug_pointwise_tiles", "sgs_debug_layer_map", "sgs_measure_fma_peak", "sgs_conv2d_sliced_i8",
     "sgs_quantize_f8", "sgs_linear_f8", "sgs_top_logits", "sgs_distill", "sgs_distill_backward", "sgs_subnet_divergence",
 ]
 
@@ -233,6 +233,7 @@ def lib():
         L.sgs_profile_read.argtypes = [vp, ci, vp, vp, vp, vp]
         L.sgs_quantize_f8.argtypes = [vp] * 7
         L.sgs_linear_f8.argtypes = [vp] * 8
+        L.sgs_debug_expire_f8_wait.argtypes = [vp] * 7 + [ci, ctypes.c_uint, vp]
         L.sgs_top_logits.argtypes = [vp] * 5
         L.sgs_distill.argtypes = [vp] * 9
         L.sgs_distill_backward.argtypes = [vp] * 8
@@ -323,6 +324,12 @@ def debug_expire_team_wait(team: int, block: int, thread: int, limit_us: int, le
     st = lib().sgs_debug_expire_team_wait(team, block, thread, limit_us, ctypes.c_void_p(left_ptr), ctypes.c_void_p(stream))
     if st != SGS_OK:
         raise SgsError(st, "sgs_debug_expire_team_wait")
+
+
+def debug_expire_f8_wait(desc: LinearF8Desc, d_x: int, d_sx: int, d_w: int, d_sw: int, d_bias: int, d_y: int, block: int, limit_us: int, stream: int = 0):
+    st = lib().sgs_debug_expire_f8_wait(ctypes.byref(desc), d_x, d_sx, d_w, d_sw, d_bias or None, d_y, block, limit_us, stream)
+    if st != SGS_OK:
+        raise SgsError(st, "sgs_debug_expire_f8_wait")
 
 
 def measure_fma_peak(stream: int = 0) -> float:

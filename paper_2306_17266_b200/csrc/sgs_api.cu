@@ -2986,8 +2986,8 @@ sgs_status_t sgs_quantize_f8(const sgs_quantize_f8_desc_t *d, const void *d_x, v
     return launched(launch_quantize_f8(a, (cudaStream_t)cuda_stream));
 } SGS_NO_THROW
 
-sgs_status_t sgs_linear_f8(const sgs_linear_f8_desc_t *d, const void *d_x, const float *d_sx, const void *d_w, const float *d_sw,
-                           const float *d_bias, void *d_y, void *cuda_stream) try {
+static sgs_status_t linear_f8(const sgs_linear_f8_desc_t *d, const void *d_x, const float *d_sx, const void *d_w, const float *d_sw,
+                              const float *d_bias, void *d_y, int withhold, unsigned long long limit_ns, void *cuda_stream) {
     if (!d || !d_x || !d_sx || !d_w || !d_sw || !d_y) return SGS_EINVAL;
     if (d->M <= 0 || d->K <= 0 || d->C <= 0 || d->K > d->Kmax || d->C > d->Cmax || d->x_format < SGS_E4M3 || d->x_format > SGS_E5M2 ||
         d->w_format < SGS_E4M3 || d->w_format > SGS_E5M2 || (d->w_block_rows != 1 && d->w_block_rows != 128) || !is_dtype(d->y_dtype) || d->act < 0 || d->act > 2)
@@ -3010,8 +3010,19 @@ sgs_status_t sgs_linear_f8(const sgs_linear_f8_desc_t *d, const void *d_x, const
     if (tc_conv_init(dev) != cudaSuccess) return SGS_ECUDA;
     a.x = d_x; a.w = d_w; a.sx = d_sx; a.sw = d_sw; a.bias = d_bias; a.y = d_y;
     a.M = d->M; a.K = d->K; a.C = d->C; a.x_e5m2 = d->x_format == SGS_E5M2; a.w_e5m2 = d->w_format == SGS_E5M2;
-    a.y_bf16 = d->y_dtype == SGS_BF16; a.act = d->act;
+    a.y_bf16 = d->y_dtype == SGS_BF16; a.act = d->act; a.withhold = withhold; a.limit_ns = limit_ns;
     return launched(launch_linear_f8(a, dev, (cudaStream_t)cuda_stream));
+}
+
+sgs_status_t sgs_linear_f8(const sgs_linear_f8_desc_t *desc, const void *d_x, const float *d_sx, const void *d_w, const float *d_sw,
+                           const float *d_bias, void *d_y, void *cuda_stream) try {
+    return linear_f8(desc, d_x, d_sx, d_w, d_sw, d_bias, d_y, -1, 0, cuda_stream);
+} SGS_NO_THROW
+
+sgs_status_t sgs_debug_expire_f8_wait(const sgs_linear_f8_desc_t *desc, const void *d_x, const float *d_sx, const void *d_w, const float *d_sw,
+                                      const float *d_bias, void *d_y, int block, unsigned limit_us, void *cuda_stream) try {
+    if (!desc || block < 0 || block >= blocks128(desc->C) || limit_us == 0 || limit_us > 1000000u) return SGS_EINVAL;
+    return linear_f8(desc, d_x, d_sx, d_w, d_sw, d_bias, d_y, block, (unsigned long long)limit_us * 1000ull, cuda_stream);
 } SGS_NO_THROW
 
 sgs_status_t sgs_top_logits(const sgs_top_logits_desc_t *d, const void *d_z, float *d_values, int *d_index, void *cuda_stream) try {

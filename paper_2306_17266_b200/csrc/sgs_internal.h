@@ -332,6 +332,8 @@ struct LinearF8Args {
     int M = 0, K = 0, C = 0;
     long long ldx = 0, ldw = 0, ldy = 0, ldsx = 0, ldsw = 0;
     int x_e5m2 = 0, w_e5m2 = 0, w_rows = 0, y_bf16 = 0, act = 0;  // w_rows: a scale for each row of w (else for 128 rows)
+    int withhold = -1;                // test of the time-out path: a block of the reduction whose w never arrives
+    unsigned long long limit_ns = 0;  // of a wait; 0: as everywhere
 };
 cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st);
 // Tensor map of a matrix of bytes: boxes of box_rows x 128 bytes, 128-byte swizzle, zeros outside.

@@ -40,6 +40,8 @@ struct F8Params {
     int act, y_bf16;
     int bulk_y;                 // columns of y that the copy unit may write: all where rows end on 16 bytes (it cuts boxes off there, not at the column)
     uint32_t formats;           // operand formats at their places in the instruction descriptor
+    int withhold;               // test of the time-out path: a block of the reduction whose w is not copied (else -1)
+    unsigned long long limit_ns;  // of a wait
 };
 
 template <int CTAS> __device__ __forceinline__ void umma_f8_if(uint32_t on, uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
@@ -105,7 +107,7 @@ __device__ __forceinline__ void copy_float(float *dst, const float *src, bool in
 }
 // Bounded wait of a converged warp, as mbar_wait but in few instructions and without a jump where the phase is complete: the warps that
 // add up wait twice in some 300 instructions.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned long long limit_ns) {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     unsigned long long t0 = 0;
 #pragma unroll 1
@@ -113,7 +115,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volati
         if (n & 255) continue;
         const unsigned long long t = global_ns();
         if (!t0) t0 = t;
-        if (__any_sync(0xffffffffu, *abort_flag || t - t0 > WAIT_LIMIT_NS)) { *abort_flag = 1; return false; }
+        if (__any_sync(0xffffffffu, *abort_flag || t - t0 > limit_ns)) { *abort_flag = 1; return false; }
     }
     return true;
 }
@@ -191,11 +193,11 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                 int m0, f0;
                 place(tile, &m0, &f0);
                 for (int b = 0; b < blocks; b++) {
-                    if (!warp_wait(&sh.empty[s], phase, abort_flag)) { ok = false; break; }
+                    if (!warp_wait(&sh.empty[s], phase, abort_flag, p.limit_ns)) { ok = false; break; }
                     const uint32_t sa = ring + (uint32_t)(s * STAGE), fb = full0 + (uint32_t)(s * 8);
                     if (rank == 0) mbar_expect_tx_if(first, smem_u32(&sh.full[s]), STAGE * CTAS);
                     tma_load_2d_if<CTAS>(on, sa, &p.tmX, fb, b * F8_BLOCK, m0);
-                    tma_load_2d_if<CTAS>(on, sa + F8_A_BYTES, &p.tmW, fb, b * F8_BLOCK, f0 + rank * B_ROWS);
+                    if (b != p.withhold) tma_load_2d_if<CTAS>(on, sa + F8_A_BYTES, &p.tmW, fb, b * F8_BLOCK, f0 + rank * B_ROWS);
                     if (++s == STAGES) { s = 0; phase ^= 1; }
                 }
             }
@@ -208,8 +210,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             bool ok = true;
             for (int tile = group; ok && tile < tiles; tile += groups)
                 for (int b = 0; b < blocks; b++) {
-                    if (!warp_wait(&sh.acc_empty[a], acc_phase, abort_flag) ||
-                        !warp_wait(&sh.full[s], phase, abort_flag)) { ok = false; break; }
+                    if (!warp_wait(&sh.acc_empty[a], acc_phase, abort_flag, p.limit_ns) ||
+                        !warp_wait(&sh.full[s], phase, abort_flag, p.limit_ns)) { ok = false; break; }
                     tc_fence_after();
                     const int steps = min(4, (p.C - b * F8_BLOCK + 31) / 32);
                     const uint32_t sa = ring + (uint32_t)(s * STAGE);
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                 int m0, f0;
                 place(tile, &m0, &f0);
                 for (int b0 = 0; b0 < blocks; b0 += F8_AHEAD) {
-                    if (!warp_wait(&sh.sc_empty[i], phase, abort_flag)) { ok = false; break; }
+                    if (!warp_wait(&sh.sc_empty[i], phase, abort_flag, p.limit_ns)) { ok = false; break; }
 #pragma unroll
                     for (int k = 0; k < F8_AHEAD; k++) {
                         if (b0 + k >= blocks) break;
@@ -275,7 +277,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             // barriers below.)
             uint32_t v[2][32];
             float rs[F8_AHEAD];
-            bool ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag);
+            bool ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag, p.limit_ns);
             tc_fence_after();
             if (ok) tmem_ld32(taddr + (uint32_t)(a * BN), v[0]);
             // (four blocks written out where registers allow: 1024x4096x4096, 29.9 us and 24.8; the pairs' kernel spills, 584 and 607 us at 8192^3)
@@ -283,7 +285,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             for (int b = 0; ok && b < blocks; b++) {
                 const int k = b % F8_AHEAD;
                 if (k == 0) {
-                    if (!(ok = warp_wait(&sh.sc_full[i], sc_phase, abort_flag))) break;
+                    if (!(ok = warp_wait(&sh.sc_full[i], sc_phase, abort_flag, p.limit_ns))) break;
                     const float4 x4 = *reinterpret_cast<const float4 *>(sh.row_scale[i][quad * 32 + lane]);
                     rs[0] = x4.x; rs[1] = x4.y; rs[2] = x4.z; rs[3] = x4.w;
                     if (!W_ROWS) {
@@ -319,7 +321,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                         }
                         if (++a == NACC) { a = 0; acc_phase ^= 1; }
                         if (b + 1 < blocks) {
-                            ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag);
+                            ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag, p.limit_ns);
                             tc_fence_after();
                             tmem_ld32(taddr + (uint32_t)(a * BN), next);
                         }
@@ -344,6 +346,10 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
                     }
                     if ((i ^= 1) == 0) sc_phase ^= 1;
                 }
+            }
+            if (!ok) {  // a wait ran out: no load of the tensor memory may be under way into registers that are used for something else now
+                tmem_ld_wait32(v[0]);
+                tmem_ld_wait32(v[1]);
             }
             // ---- bias, activation, one rounding, output
             half_sync();  // (all have read the last tile's)
@@ -466,10 +472,10 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, 2) linear_f8_split_kernel(co
         int s = 0;
         uint32_t phase = 1;
         for (int b = 0; b < blocks; b++) {
-            if (!warp_wait(&sh.empty[s], phase, abort_flag)) break;
+            if (!warp_wait(&sh.empty[s], phase, abort_flag, p.limit_ns)) break;
             const uint32_t sa = ring + (uint32_t)(s * STAGE), fb = full0 + (uint32_t)(s * 8);
             mbar_expect_tx_if(on, fb, STAGE);
-            tma_load_2d_if<1>(on, sa, &p.tmW, fb, (b_first + b) * F8_BLOCK, f0);
+            if (b_first + b != p.withhold) tma_load_2d_if<1>(on, sa, &p.tmW, fb, (b_first + b) * F8_BLOCK, f0);
             tma_load_2d_if<1>(on, sa + F8_A_BYTES, &p.tmX, fb, (b_first + b) * F8_BLOCK, n0);
             if (++s == STAGES) { s = 0; phase ^= 1; }
         }
@@ -480,7 +486,7 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, 2) linear_f8_split_kernel(co
         int s = 0, a = 0;
         uint32_t phase = 0, acc_phase = 1;
         for (int b = 0; b < blocks; b++) {
-            if (!warp_wait(&sh.acc_empty[a], acc_phase, abort_flag) || !warp_wait(&sh.full[s], phase, abort_flag)) break;
+            if (!warp_wait(&sh.acc_empty[a], acc_phase, abort_flag, p.limit_ns) || !warp_wait(&sh.full[s], phase, abort_flag, p.limit_ns)) break;
             tc_fence_after();
             const int steps = min(4, (p.C - (b_first + b) * F8_BLOCK + 31) / 32);
             const uint32_t sa = ring + (uint32_t)(s * STAGE);
@@ -497,7 +503,7 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, 2) linear_f8_split_kernel(co
         int i = 0;
         uint32_t phase = 1;
         for (int b0 = 0; b0 < blocks; b0 += F8_AHEAD) {
-            if (!warp_wait(&sh.sc_empty[i], phase, abort_flag)) break;
+            if (!warp_wait(&sh.sc_empty[i], phase, abort_flag, p.limit_ns)) break;
 #pragma unroll
             for (int k = 0; k < F8_AHEAD; k++) {
                 if (b0 + k >= blocks) break;
@@ -525,10 +531,10 @@ __global__ void __launch_bounds__(F8_SPLIT_THREADS, 2) linear_f8_split_kernel(co
         for (int b = 0; b < blocks; b++) {
             const int k = b % F8_AHEAD;
             if (k == 0) {
-                ok = ok && warp_wait(&sh.sc_full[i], sc_phase, abort_flag);
+                ok = ok && warp_wait(&sh.sc_full[i], sc_phase, abort_flag, p.limit_ns);
                 w4 = *reinterpret_cast<const float4 *>(sh.w_scale[i][W_ROWS ? l : 0]);
             }
-            if (ok && (ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag))) {
+            if (ok && (ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag, p.limit_ns))) {
                 const float f = k & 2 ? (k & 1 ? w4.w : w4.z) : (k & 1 ? w4.y : w4.x);
                 const float2 f2 = make_float2(f, f);
                 tc_fence_after();
@@ -696,7 +702,7 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
     p.sx = a.sx; p.sw = a.sw; p.bias = a.bias; p.y = a.y; p.status = tc_status_word(device);
     p.ldsx = a.ldsx; p.ldsw = a.ldsw; p.ldy = a.ldy;
     p.M = a.M; p.K = a.K; p.C = a.C; p.blocks = (a.C + F8_BLOCK - 1) / F8_BLOCK;
-    p.act = a.act; p.y_bf16 = a.y_bf16;
+    p.act = a.act; p.y_bf16 = a.y_bf16; p.withhold = a.withhold; p.limit_ns = a.limit_ns ? a.limit_ns : WAIT_LIMIT_NS;
     const size_t pitch = (size_t)a.ldy * (a.y_bf16 ? 2 : 4);
     const int unit = a.y_bf16 ? 8 : 4;  // elements of 16 bytes
     if (((reinterpret_cast<uintptr_t>(a.y) | pitch) & 15) == 0 && tc_encode_output(&p.tmY, a.y, (uint64_t)a.K, (uint64_t)a.M, pitch, a.y_bf16, 4 * unit, 32))
