@@ -13,6 +13,7 @@
 #include "sgs_pdl.cuh"
 
 #include <algorithm>
+#include <cmath>
 
 namespace sgs {
 namespace {
@@ -447,7 +448,7 @@ struct DisParams {
     int V, k, backward, parts, table;  // table: places of the table of classes, a power of two
     long long ldz, lddz, ldt;
     float inv_t, temperature;
-    double grad_factor;  // grad_scale * temperature: in 64 bits, since it may leave fp32's range where its product with a row's scale does not
+    float grad_factor[3];  // their product is grad_scale * temperature, which may leave fp32's range where its product with a row's scale does not
 };
 
 // A team of TEAM threads takes a row (or a cluster's part of one): a block, or for short rows a warp, eight to a block.
@@ -560,13 +561,12 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
         stud = warp_join(stud, a);
         cluster_arrive();  // (nobody leaves before all have read: the wait is at the end)
     }
-    // The running maximum leaves NaN out, the sum does not: a row whose sum is NaN has a NaN (or plus infinity) among its logits.  A row is
-    // empty where its sum is 0, not where the largest of its numbers is minus infinity: beside that there may be a NaN.
-    const float logsum = p.backward ? kept.y : logf(stud.y);
-    const float zmax = p.backward ? kept.x : logsum == logsum || stud.x == -NEG_INF ? stud.x : logsum;
+    // The running maximum leaves NaN out, the sum does not.  A row is empty where its sum is 0, not where the largest of its numbers is minus
+    // infinity: beside that there may be a NaN.
+    const float zmax = p.backward ? kept.x : stud.x, logsum = p.backward ? kept.y : logf(stud.y);
     const float base = zmax == NEG_INF ? 0.f : zmax, off = logsum == NEG_INF ? 0.f : logsum;
     const float tmax = teach.x == NEG_INF ? 0.f : teach.x, tsum = teach.y;
-    const float c = used ? (float)(p.grad_factor * (double)row_scale) : 0.f, off2 = off * LOG2E;
+    const float c = used ? row_scale * p.grad_factor[0] * p.grad_factor[1] * p.grad_factor[2] : 0.f, off2 = off * LOG2E;
     float loss = 0.f;
     const float log_tsum = logf(tsum);
 #pragma unroll
@@ -644,7 +644,10 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
         }
         if (t == 0) {
             p.loss[r] = used ? loss * p.temperature : 0.f;
-            if (p.stat) { p.stat[2 * r] = zmax; p.stat[2 * r + 1] = logsum; }
+            if (p.stat) {
+                p.stat[2 * r] = logsum == logsum || zmax == -NEG_INF ? zmax : logsum;  // (NaN in a row with a NaN)
+                p.stat[2 * r + 1] = logsum;
+            }
         }
     }
     if (meet) cluster_wait();
@@ -705,7 +708,16 @@ cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
     DisParams p;
     p.z = a.z; p.dz = a.dz; p.teacher = a.teacher; p.row_scale = a.row_scale; p.index = a.index; p.loss = a.loss; p.stat = a.stat;
     p.V = a.classes; p.k = a.top; p.backward = a.backward; p.ldz = a.ldz; p.lddz = a.lddz; p.ldt = a.ldt;
-    p.inv_t = 1.f / a.temperature; p.temperature = a.temperature; p.grad_factor = (double)a.grad_scale * a.temperature;
+    p.inv_t = 1.f / a.temperature; p.temperature = a.temperature;
+    // (a number of fp32's precision and powers of two, all of them above 1 or all below: a row's scale comes to the product without leaving the
+    // range on the way; multiplied in 64 bits by every thread a row of 65536 takes 0.7 % longer)
+    int e;
+    p.grad_factor[0] = (float)std::frexp((double)a.grad_scale * a.temperature, &e);  // (e from -297 to 256)
+    for (int i = 0; i < 3; i++) {
+        const int part = std::max(-100, std::min(100, e));
+        p.grad_factor[i] = std::ldexp(i ? 1.f : p.grad_factor[0], part);
+        e -= part;
+    }
     const double bytes = (double)a.classes * (a.bf16 ? 2 : 4);
     p.parts = parts_for(a.rows, bytes, 16384);
     return a.bf16 ? launch_distill_type<__nv_bfloat16>(p, a.rows, bytes, st) : launch_distill_type<float>(p, a.rows, bytes, st);
