@@ -9,8 +9,8 @@
 // Three forms, by the size of the call (the rule stands at the launch): pairs of blocks on tiles of 256 x 256, single blocks on tiles of
 // 128 x 128, and for few rows, or few tiles and a long reduction, tiles of 128 rows of w whose reduction a cluster shares.
 //
-// What bounds the large form (8192^3, 585 us, 1.88 PFLOP/s at some 1.55 GHz under the power cap): the way of a block's sums through the
-// warps.  The MMAs of a block take 512 clocks; with the sums left out a block takes 745 (operand copies and MMAs share the port of shared
+// What bounds the large form (8192^3, 579 us, 1.90 PFLOP/s at some 1.55 GHz under the power cap; 574 to 594 from call to call): the way of a
+// block's sums through the warps.  The MMAs of a block take 512 clocks; with the sums left out a block takes 745 (operand copies and MMAs share the port of shared
 // memory, and each accumulator passes from hand to hand), with them 1030: a wait, four loads of the tensor memory and 64 packed
 // multiply-adds are a chain that two warps a scheduler do not hide.  Measured instead (same call, 598 us then): sixteen warps of 64 columns
 // 602 us; tiles of 256 x 192 with twelve warps that read all their columns first 610 us; 256 x 160 with three accumulators 676 us; two teams
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
             bool ok = warp_wait(&sh.acc_full[a], acc_phase, abort_flag, p.limit_ns);
             tc_fence_after();
             if (ok) tmem_ld32(taddr + (uint32_t)(a * BN), v[0]);
-            // (four blocks written out where registers allow: 1024x4096x4096, 29.9 us and 24.8; the pairs' kernel spills, 584 and 607 us at 8192^3)
+            // (four blocks written out where registers allow: 1024x4096x4096, 29.9 us and 24.8; the pairs' kernel spills, 607 us at 8192^3)
 #pragma unroll(CTAS == 1 ? F8_AHEAD : 1)
             for (int b = 0; ok && b < blocks; b++) {
                 const int k = b % F8_AHEAD;
@@ -426,8 +426,8 @@ __global__ void __launch_bounds__(F8_THREADS, 1) linear_f8_kernel(const __grid_c
 
 // Few rows of x: the rows of w take the lanes (128 a block), up to N rows of x the columns, and the blocks of a cluster share the
 // reduction, whose parts meet in distributed shared memory, in the order of c.  What bounds such a call is w's bytes: 16 KB of them a
-// stage, two thread blocks an SM (one row, 8192 filters, 4096 channels: 9.2 us, 3.6 TB/s; 16384 x 8192: 57 % of the DRAM rate; the rest is
-// the way in and out: launch, first copies, the cluster's two meetings).  Blocks that share an SM hold 256 columns of tensor memory at most
+// stage, two thread blocks an SM (one row, 8192 filters, 4096 channels: 9.3 us, 3.6 TB/s; 16384 x 8192: 25.7 us, 5.2 TB/s; the weights of
+// several calls in turn, 268 MB in all; the rest is the way in and out: launch, first copies, the cluster's two meetings).  Blocks that share an SM hold 256 columns of tensor memory at most
 // each, and kernels that fit beside them the rest: no allocation waits for another block's, which a cluster whose blocks wait for each
 // other could not afford.  Warp 0 loads, 1 issues, 2 brings the scales, warps 4..7 add up, a quadrant of the lanes each.
 constexpr int F8_SPLIT_THREADS = 256, F8_SPLIT_RING = 96 * 1024;
@@ -710,14 +710,16 @@ cudaError_t launch_linear_f8(const LinearF8Args &a, int device, cudaStream_t st)
     p.formats = ((uint32_t)(a.x_e5m2 ? 1 : 0) << 7) | ((uint32_t)(a.w_e5m2 ? 1 : 0) << 10);
     const long long tiles = (long long)((a.M + 127) / 128) * ((a.K + 127) / 128);
     // Few rows split the reduction over clusters.  So do more than 32 where the tiles of 128 x 128 would leave three SMs in four idle and the
-    // reduction is long enough to pay for the meeting (split and in tiles, us: 128 x 4096 x 4096 11.1 and 13.3, 300 x 1000 x 8192 14.0 and
-    // 21.8; 256 x 4096 x 4096, 64 tiles, 15.5 and 13.6; 128 x 4096 x 1024 7.0 and 6.0, 64 x 320 x 640 6.5 and 5.0).
+    // reduction is long enough to pay for the meeting (split and in tiles, us: 128 x 4096 x 4096 10.8 and 13.4, 300 x 1000 x 8192 14.0 and
+    // 22.0; with 64 tiles 256 x 4096 x 4096, which the split form reads w four times for, 15.2 and 13.4, and 64 x 8192 x 4096, which it would
+    // read once, 12.2 and 13.6; 128 x 4096 x 1024 6.9 and 6.0, 64 x 320 x 640 6.6 and 4.9).
     if (a.M <= 16) return a.w_rows ? launch_split<16, true>(p, a, g_set[4], st) : launch_split<16, false>(p, a, g_set[5], st);
     if (a.M <= 32) return a.w_rows ? launch_split<32, true>(p, a, g_set[6], st) : launch_split<32, false>(p, a, g_set[7], st);
     if (tiles * 4 <= sm_count() && p.blocks > 8) return a.w_rows ? launch_split<64, true>(p, a, g_set[8], st) : launch_split<64, false>(p, a, g_set[9], st);
     // Pairs of SMs take a tile of 256 x 256 in 1.6 times the time that one takes for 128 x 128 (4096 long: 16.5 us more for each wave, and
-    // 10.2): they win where they need that many fewer waves.  1024 x 4096, one wave and two, 22.5 and 24.5 us; 1280 x 4096, two and three,
-    // 38.7 and 33.6; 512 x 4096, one and one, 21.4 and 14.2; 50176 x 64, 256 long, three and three, 11.6 and 9.0.
+    // 10.2): they win where they need that many fewer waves.  1024 x 4096, one wave and two, 22.1 and 23.9 us; 1280 x 4096, two and three,
+    // 39.0 and 33.4; 512 x 4096, one and one, 21.4 and 13.9; 50176 x 64, 256 long, three and three, 11.7 and 9.1; 12544 x 408, 512 long, two
+    // and three, 12.6 and 10.6.  (Both count whole tiles: of 408 filters' fourth one 24 are in use.)
     const long long sms = sm_count(), pair_tiles = (long long)((a.M + 255) / 256) * ((a.K + 255) / 256);
     const long long waves = (tiles + sms - 1) / sms, pair_waves = (pair_tiles + sms / 2 - 1) / (sms / 2);
     const bool pairs = 8 * pair_waves <= 5 * waves;

@@ -5,10 +5,10 @@
 // through distributed shared memory where the rows alone do not fill the GPU; copies of 16 bytes into shared memory run ahead of their
 // use, from the first aligned element of a row on (rows of an odd pitch start anywhere); and a second pass reads a row again instead of
 // keeping it: two blocks an SM are between their passes with 39 MB of rows of 128 KB, which stay in the 126 MB L2 (four blocks an SM, and
-// what they write, do not: 2048 x 65536 bf16 takes 123 us then, 110 with two).
-// Measured (B200): top 64 of 512 x 131071 bf16 31.8 us (4.2 TB/s), fp32 51 us (5.2 TB/s); loss and gradient of 2048 x 65536 bf16 110 us
-// (4.9 TB/s of what has to be read and written), fp32 201 us (5.4 TB/s); the loss alone 52 us; the gradient of 1000 x 100008 bf16 71.5 us
-// (5.6 TB/s); the loss of 64 x 1000 fp32 3.1 us.
+// what they write, do not: 2048 x 65536 bf16 takes 121 us then, 113 with two).
+// Measured (B200): top 64 of 512 x 131071 bf16 32.4 us (4.1 TB/s), fp32 52.7 us (5.1 TB/s), top 32 of 8192 x 1000 fp32 39 us; loss and
+// gradient of 2048 x 65536 bf16 113 us (4.8 TB/s of what has to be read and written; 110 where a sixteenth of the rows have no list), fp32
+// 200 us (5.4 TB/s); the loss alone 50 and 84 us; the gradient of 1000 x 100008 bf16 72.4 us (5.5 TB/s); the loss of 64 x 1000 fp32 3.2 us.
 #include "sgs_internal.h"
 #include "sgs_pdl.cuh"
 
@@ -596,8 +596,8 @@ template <typename T, int TEAM, int BLOCK> __global__ void __launch_bounds__(BLO
             }
             named[q] = c * (pow2((zl[q] - base) * a - off2) - sum);
         }
-        // fp32 rows: what is read for the last time and what is written make way in L2 for the rows between their passes (2048 x 65536: 233 us,
-        // 198 with it; bf16 rows, which the exponentials bound as much as the bytes do, take 112 and 115 us)
+        // fp32 rows: what is read for the last time and what is written make way in L2 for the rows between their passes (2048 x 65536: 239 us,
+        // 200 with it; bf16 rows, half as many bytes in L2, take 113 and 131 us)
         constexpr bool FIRST_OUT = sizeof(T) == 4;
         const bool same = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
         const float2 a2 = make_float2(a, a), base2 = make_float2(-base, -base), less2 = make_float2(-off2, -off2), c2 = make_float2(c, c);
@@ -661,21 +661,22 @@ template <typename T, int TEAM, int BLOCK> cudaError_t launch_distill_blocks(con
     return launch_pdl(distill_kernel<T, TEAM, BLOCK>, grid, dim3(BLOCK), RING + list, st, (unsigned)p.parts, p, rows);
 }
 template <typename T> cudaError_t launch_distill_type(DisParams &p, int rows, double bytes, cudaStream_t st) {
-    // Lists of up to 128 slots are compared with each other outright (64 of 4096 classes, 16384 rows: 66 us, 98 with the table; 1000 of
-    // 1000, 64 rows: 35 us, 6 with it).
+    // Lists of up to 128 slots are compared with each other outright (64 of 4096 classes, 16384 rows: 69 us, 99 with the table; 1000 of
+    // 1000, 64 rows: 44 us, 5.2 with it).
     p.table = 0;
     if (p.dz && p.k > 128)
         for (p.table = 2; p.table < 2 * p.k; p.table *= 2) {}
     const unsigned list = (unsigned)(p.k * 8 + p.table * 4);
-    // Short rows, and many of them: a warp each.
+    // Short rows, and many of them: a warp each (loss and gradient of 16384 x 4096 bf16: 69 us, 166 with a block a row; the loss of 16384 x 1000
+    // fp32: 20.5 and 100 us).
     if (bytes <= 8192 && p.k <= 128 && rows >= 8 * sm_count()) {
         constexpr int TEAMS = 256 / 32;
         p.parts = 1;
         return launch_distill_blocks<T, 32, 256>(p, dim3((unsigned)(((long long)rows + TEAMS - 1) / TEAMS)), TEAMS * list, rows, st);
     }
     // Blocks of 256 threads keep four rows of an SM at work, which serves the loss alone; with a gradient the rows between their two
-    // passes have to stay in L2 together with what is written: blocks of 512, two rows an SM (2048 x 65536 bf16: 123 and 109 us; the loss
-    // alone 58 and 62 us).
+    // passes have to stay in L2 together with what is written: blocks of 512, two rows an SM (2048 x 65536 bf16: 121 and 113 us; the loss
+    // alone 50 and 60 us).
     const dim3 grid((unsigned)rows, 1, (unsigned)p.parts);
     if (p.dz && bytes / p.parts > 16384) return launch_distill_blocks<T, 512, 512>(p, grid, list, rows, st);
     return launch_distill_blocks<T, 256, 256>(p, grid, list, rows, st);
@@ -698,9 +699,9 @@ cudaError_t launch_top_logits(const TopArgs &a, cudaStream_t st) {
     TopParams p;
     p.z = a.z; p.values = a.values; p.index = a.index; p.V = a.classes; p.k = a.top; p.ldz = a.ldz; p.ldt = a.ldt;
     const double bytes = (double)a.classes * (a.bf16 ? 2 : 4);
-    // (a cluster's two meetings cost as much as 64 KB of a row: 64 x 32768 bf16 takes 10.6 us with a block a row, 12.9 with two)
+    // (a cluster's two meetings cost as much as 64 KB of a row: 64 x 32768 bf16 takes 6.7 us with a block a row, 9.2 with two)
     p.parts = parts_for(a.rows, bytes, 65536);
-    // Many short rows: blocks of 128 threads, eight an SM (8192 x 1000 fp32: 94 us with 512 threads, 48 with 128; 64 x 1000: 4.4 and 5.4 us).
+    // Many short rows: blocks of 128 threads, eight an SM (8192 x 1000 fp32: 126 us with 512 threads, 39 with 128; 64 x 1000: 4.4 and 5.5 us).
     return a.bf16 ? launch_top_type<__nv_bfloat16>(p, a.rows, bytes, st) : launch_top_type<float>(p, a.rows, bytes, st);
 }
 

@@ -11,8 +11,10 @@
 // threads a row, so the largest of a row is a shuffle among 16 lanes, and the 8 codes of a column and thread are one 8-byte word
 // of the transposed tile, which goes through shared memory (16 KB, units of 8 bytes swizzled by the column group: neither the
 // writes nor the 16-byte reads meet in a bank) so that the transposed codes leave in rows of 128 bytes too.
-// Measured (B200, 8192 x 8192 bf16): row-wise 32.2 us (6.3 TB/s), transposed 37.3 us (5.4 TB/s), both 58.4 us (4.7 TB/s: the integer pipe is
-// busy 59 % of the time, shared memory 48 %); fp32, both sides, 96 us (4.3 TB/s).
+// Measured (B200, 8192 x 8192, row-wise / transposed / both from one read, us): bf16 32.3 / 37.6 / 58.6 (6.3, 5.4, 4.7 TB/s), fp32 62.0 / 60.5 /
+// 95.3 (5.5, 5.6, 4.3 TB/s); with blocks of 128 x 128 bf16 34.4 / 34.5 / 47.0, fp32 58.8 / 55.5 / 64.5 (6.2 TB/s).  Both sides at once are not
+// held by one unit (integer pipe 59 %, DRAM 49 %, shared memory 48 %): a block has one tile, whose load, exchange of maxima, codes and
+// transpose follow each other; without the columns' maxima, with blocks of 128 x 128, it is a fifth faster.
 #include "sgs_internal.h"
 #include "sgs_pdl.cuh"
 
