@@ -460,6 +460,14 @@ EncodeTiledFn encode_fn() {
     });
     return fn;
 }
+// The call itself.  It wants the device's context bound to the host thread, which the runtime does with a thread's first launch or allocation:
+// where this comes before one, the device is set here.
+template <typename... A> CUresult encode_tiled(A... args) {
+    CUresult r = encode_fn()(args...);
+    int dev = 0;
+    if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) r = encode_fn()(args...);
+    return r;
+}
 
 // Encoded tensor maps by their defining numbers.  A SubNet never seen before still slices the same stored layers
 // into one of a few (K', C') boxes and reads the same workspaces at one of a few channel counts, so most of its
@@ -497,7 +505,7 @@ bool encode_map(CUtensorMap *m, const void *base, int rank, const uint64_t *dims
     cuuint32_t bx[5], es[5];
     for (int i = 0; i < rank; i++) { gd[i] = dims[i]; bx[i] = box[i]; es[i] = 1; }
     for (int i = 0; i + 1 < rank; i++) gs[i] = strides_bytes[i];
-    CUresult r = encode_fn()(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), gd, gs, bx, es,
+    CUresult r = encode_tiled(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), gd, gs, bx, es,
                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return false;
@@ -528,7 +536,7 @@ bool tc_encode_output(CUtensorMap *m, void *base, uint64_t cols, uint64_t rows, 
     if (!encode_fn()) return false;
     const cuuint64_t gd[2] = {cols, rows}, gs[1] = {pitch};
     const cuuint32_t bx[2] = {box_cols, box_rows}, es[2] = {1, 1};
-    return encode_fn()(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return encode_tiled(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                        CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -536,7 +544,7 @@ bool tc_encode_bytes(CUtensorMap *m, const void *base, uint64_t cols, uint64_t r
     if (!encode_fn()) return false;
     const cuuint64_t gd[2] = {cols, rows}, gs[1] = {pitch};
     const cuuint32_t bx[2] = {128, box_rows}, es[2] = {1, 1};
-    return encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
