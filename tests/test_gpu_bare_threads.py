@@ -20,7 +20,7 @@ codes = lambda *s: torch.randint(0, 0x70, s, generator=torch.Generator(device="c
 def both(call, outs):
     """call() in a thread of its own, then in this one: the outputs of the two."""
     torch.cuda.synchronize()
-    errors, got = [], []
+    errors = []
 
     def work():
         try:
